@@ -656,6 +656,122 @@ int op_im2col7(int32_t n, int32_t h, int32_t w, int32_t ho, int32_t wo, int32_t 
 int op_maxpool(int32_t backward, int32_t n, int32_t h, int32_t w, int32_t c, int32_t ho, int32_t wo,
                const float *g, const void *r, const void *y, void *out, void *arg, void *stream);
 
+/* ---- group norm and dropout ---------------------------------------------
+ * The unit of a checkpointed net whose statistics do not couple its batch:
+ * group norm, an activation and dropout over channels-last tensors, forward,
+ * re-run and backward, and dropout alone (with a residual).  They keep to the
+ * conventions of the operator calls above, except that channel counts are
+ * free.
+ *
+ * Tensors are n samples of hw pixels of c channels (rows of hidden states: hw
+ * = 1), bf16 or f32, `ld` elements between consecutive pixels (0: c; larger
+ * for a channel slice of a wider tensor; elements between the rows are neither
+ * read nor written).  Everything is computed in fp32 and rounded once.  Channel
+ * counts that 8 divides take accesses of eight elements (at any address and
+ * stride); others are served element by element.
+ * Outputs may be written over an input of the same type and stride (y over x;
+ * d over g or x); other overlaps are not allowed.  The stream belongs to the
+ * current device.
+ */
+#define CKPT_TYPE_F32  0
+#define CKPT_TYPE_BF16 1
+
+#define CKPT_ACT_NONE 0 /* v = u                */
+#define CKPT_ACT_RELU 1 /* v = max(u, 0)        */
+#define CKPT_ACT_SILU 2 /* v = u / (1 + exp(-u)) */
+
+/*
+ * Dropout from a counter-based generator: the mask is a function of (seed,
+ * step, site, element), so a re-run and a backward form the first forward's
+ * mask again and nothing stores it.
+ *   rng   device, two uint64, 8-byte aligned: seed and step, read when the
+ *         kernel runs: a program that captured the call writes the next step's
+ *         number there between replays
+ *   site  which dropout of the network this is
+ *   p     probability of dropping, in [0, 1].  T = floor(65536 p + 1/2);
+ *         kept elements are scaled by 65536 / (65536 - T), so the mean is exact
+ *         for the probability T / 65536 that is met.
+ * Element e of the tensor in row-major order ((sample hw + pixel) c + channel,
+ * whatever the strides) is kept iff the 16-bit half e % 8 (bits 16 (h % 2) of
+ * word h / 2) of Philox4x32-10 (Salmon et al., SC 2011) with key = seed and
+ * counter words e / 8, site, step low, step high is at least T.  A dropped
+ * element is 0 whatever its value was.
+ */
+typedef struct ckpt_dropout {
+  const uint64_t *rng;
+  uint32_t site;
+  uint32_t reserved;
+  double p;
+} ckpt_dropout;
+
+/* A group norm: n samples of hw pixels of c channels in `groups` groups of
+ * consecutive channels; xtype: x and y; gtype: g; dtype: d (an f32 x takes f32
+ * g and d).  eps is added to the variance (> 0). */
+typedef struct ckpt_gn_desc {
+  int64_t n, hw;
+  int32_t c, groups;
+  int32_t act;
+  int32_t xtype, gtype, dtype;
+  int64_t ldx, ldy, ldg, ldd;
+  float eps;
+  int32_t reserved;
+} ckpt_gn_desc;
+
+/* op_gn_workspace_bytes -- device workspace op_gn_forward (backward = 0) or
+ * op_gn_backward needs for this problem, 0 for none (a null workspace
+ * will do).  Calls that share one must not overlap.
+ * Errors: CKPT_E_INVALID for sizes below 1, groups that do not divide c, an
+ * unknown activation or type, a stride below c, eps <= 0; CKPT_E_UNSUPPORTED
+ * for n hw c >= 2^35, n groups >= 2^25, or more than 1024 channels per group
+ * (up to 4096 are served where 8 divides them). */
+int op_gn_workspace_bytes(const ckpt_gn_desc *desc, int32_t backward, uint64_t *bytes);
+
+/*
+ * op_gn_forward -- st = mean | 1/sqrt(biased variance + eps), each [n groups]
+ * f32, of every sample and group, and y = dropout(act(u)) with u = (x - mean)
+ * (gamma rstd) + beta; gamma, beta f32 [c]; drop null for no dropout.  The
+ * variance is the mean of squared differences from the mean (no cancellation
+ * for a mean far from zero).
+ * Errors: as op_gn_workspace_bytes; CKPT_E_INVALID for null pointers, a p
+ * outside [0, 1], an address that is not a multiple of its element's size or a
+ * workspace not 16-byte aligned; CKPT_E_WORKSPACE for a short one.
+ */
+int op_gn_forward(const ckpt_gn_desc *desc, const void *x, const float *gamma, const float *beta,
+                  const ckpt_dropout *drop, void *y, float *st, void *workspace,
+                  uint64_t workspace_bytes, void *stream);
+
+/* op_gn_apply -- the same y, bit for bit, from statistics st that op_gn_forward
+ * left: what a checkpointed segment's re-run needs (one pass over x). */
+int op_gn_apply(const ckpt_gn_desc *desc, const void *x, const float *st, const float *gamma,
+                const float *beta, const ckpt_dropout *drop, void *y, void *stream);
+
+/*
+ * op_gn_backward -- for g = dL/dy, from x and st alone (activation and mask are
+ * formed again): with du = dropout(g) act'(u), xhat = (x - mean) rstd and means
+ * over each group of a sample, dbeta = sum du, dgamma = sum du xhat (f32 [c]),
+ * d = rstd (gamma du - mean(gamma du) - xhat mean(gamma du xhat)).  ReLU's
+ * derivative is taken at the u the forward formed, 0 at u = 0.  Sums are added
+ * in a fixed order: the same bits on every run.
+ * Errors: as op_gn_forward; CKPT_E_UNSUPPORTED for an f32 x with bf16 g or d.
+ */
+int op_gn_backward(const ckpt_gn_desc *desc, const void *g, const void *x, const float *st,
+                   const float *gamma, const float *beta, const ckpt_dropout *drop, void *d,
+                   float *dgamma, float *dbeta, void *workspace, uint64_t workspace_bytes,
+                   void *stream);
+
+/*
+ * op_dropout -- y [rows, cols] = dropout(x) + res (res null: none; of y's type).
+ * Its backward is the same call on the gradient, without res.  x, res, y with
+ * row strides ldx, ldr, ldy (0: cols); y may be written over x (same type and
+ * stride) or res.
+ * Errors: CKPT_E_INVALID for sizes below 1, null x, y, drop or rng, unknown
+ * types, a stride below cols, a p outside [0, 1] or a misaligned address;
+ * CKPT_E_UNSUPPORTED for rows cols >= 2^35.
+ */
+int op_dropout(int64_t rows, int64_t cols, int32_t xtype, const void *x, int64_t ldx, const void *res,
+               int64_t ldr, int32_t ytype, void *y, int64_t ldy, const ckpt_dropout *drop,
+               void *stream);
+
 /* ckpt_last_error -- message of the last failed call on this thread ("" if
  * none). */
 const char *ckpt_last_error(void);

@@ -152,12 +152,36 @@ _sig("op_bnb_backward_apply", C.c_int, [C.c_int64, C.c_int32, _vp, _vp, _vp, _vp
 _sig("op_im2col7", C.c_int, [C.c_int32] * 6 + [_vp, _vp, _vp])
 _sig("op_maxpool", C.c_int, [C.c_int32] * 7 + [_vp, _vp, _vp, _vp, _vp, _vp])
 
+
+
+class Dropout(C.Structure):
+    _fields_ = [("rng", C.c_void_p), ("site", C.c_uint32), ("reserved", C.c_uint32), ("p", C.c_double)]
+
+
+class GnDesc(C.Structure):
+    _fields_ = ([(k, C.c_int64) for k in ("n", "hw")] +
+                [(k, C.c_int32) for k in ("c", "groups", "act", "xtype", "gtype", "dtype")] +
+                [(k, C.c_int64) for k in ("ldx", "ldy", "ldg", "ldd")] +
+                [("eps", C.c_float), ("reserved", C.c_int32)])
+
+
+_gnp, _drp = C.POINTER(GnDesc), C.POINTER(Dropout)
+_sig("op_gn_workspace_bytes", C.c_int, [_gnp, C.c_int32, _u64p])
+_sig("op_gn_forward", C.c_int, [_gnp, _vp, _vp, _vp, _drp, _vp, _vp, _vp, C.c_uint64, _vp])
+_sig("op_gn_apply", C.c_int, [_gnp, _vp, _vp, _vp, _vp, _drp, _vp, _vp])
+_sig("op_gn_backward", C.c_int, [_gnp, _vp, _vp, _vp, _vp, _vp, _drp, _vp, _vp, _vp, _vp, C.c_uint64, _vp])
+_sig("op_dropout", C.c_int, [C.c_int64, C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, _vp,
+                             C.c_int64, _drp, _vp])
+
+TYPE_F32, TYPE_BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 EPI_STORE, EPI_ADD, EPI_BF16STATS, EPI_ADDMASK, EPI_BNBWD = 0, 1, 3, 4, 6
 BNB_RES_NONE, BNB_RES_ID, BNB_RES_BN = 0, 1, 2
 
 EXPORTED = ["op_gemm_bf16_blocks", "op_gemm_bf16", "op_sum_partials", "op_conv_bf16_fwd",
             "op_conv_bf16_dgrad", "op_conv_bf16_wgrad", "op_bn_finalize", "op_bnb_partial_blocks",
             "op_bnb_apply", "op_bnb_backward", "op_bnb_backward_apply", "op_im2col7", "op_maxpool",
+            "op_gn_workspace_bytes", "op_gn_forward", "op_gn_apply", "op_gn_backward", "op_dropout",
             "ckpt_last_error", "plan_checkpoints", "plan_info", "plan_cuts", "plan_serialize",
             "plan_free", "plan_search", "graph_plan", "graph_plan_info", "graph_plan_schedule",
             "graph_plan_blocks", "graph_plan_free", "net_node_graph", "graph_workspace_bytes",
@@ -621,3 +645,59 @@ def op_im2col7(n, h, w, ho, wo, x, col, kp=147, stream=None):
 def op_maxpool(backward, n, h, w, c, ho, wo, r, out, g=None, y=None, arg=None, stream=None):
     _check(_lib.op_maxpool(int(backward), n, h, w, c, ho, wo, _addr(g), _addr(r), _addr(y), _addr(out),
                            _addr(arg), _s(stream)))
+
+
+# ------------------------------------------------- group norm and dropout --
+def type_of(t) -> int:
+    """The type code of a torch tensor."""
+    codes = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+    if t.dtype not in codes:
+        raise CkptError(E_UNSUPPORTED, f"tensors are float32 or bfloat16, not {t.dtype}")
+    return codes[t.dtype]
+
+
+def dropout(rng, p: float, site: int = 0) -> Dropout:
+    """Dropout with the {seed, step} pair at `rng` (device int64 or uint64 [2],
+    kept alive by the result)."""
+    d = Dropout(_addr(rng), site, 0, p)
+    d._keep = rng
+    return d
+
+
+def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=None, ldx=0, ldy=0, ldg=0, ldd=0,
+            eps=1e-5) -> GnDesc:
+    """gtype and dtype default to xtype, strides to c."""
+    return GnDesc(n, hw, c, groups, act, xtype, xtype if gtype is None else gtype, xtype if dtype is None else dtype,
+                  ldx, ldy, ldg, ldd, eps, 0)
+
+
+def _byref(x):
+    return None if x is None else C.byref(x)
+
+
+def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
+    v = C.c_uint64()
+    _check(_lib.op_gn_workspace_bytes(_byref(desc), int(backward), C.byref(v)))
+    return v.value
+
+
+def op_gn_forward(desc, x, gamma, beta, y, st, workspace=None, workspace_bytes=0, drop=None, stream=None):
+    _check(_lib.op_gn_forward(_byref(desc), _addr(x), _addr(gamma), _addr(beta), _byref(drop), _addr(y), _addr(st),
+                              _addr(workspace), int(workspace_bytes), _s(stream)))
+
+
+def op_gn_apply(desc, x, st, gamma, beta, y, drop=None, stream=None):
+    _check(_lib.op_gn_apply(_byref(desc), _addr(x), _addr(st), _addr(gamma), _addr(beta), _byref(drop), _addr(y),
+                            _s(stream)))
+
+
+def op_gn_backward(desc, g, x, st, gamma, beta, d, dgamma, dbeta, workspace=None, workspace_bytes=0, drop=None,
+                   stream=None):
+    _check(_lib.op_gn_backward(_byref(desc), _addr(g), _addr(x), _addr(st), _addr(gamma), _addr(beta), _byref(drop),
+                               _addr(d), _addr(dgamma), _addr(dbeta), _addr(workspace), int(workspace_bytes),
+                               _s(stream)))
+
+
+def op_dropout(rows, cols, x, y, drop, res=None, xtype=TYPE_BF16, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
+    _check(_lib.op_dropout(rows, cols, xtype, _addr(x), ldx, _addr(res), ldr, xtype if ytype is None else ytype,
+                           _addr(y), ldy, _byref(drop), _s(stream)))
