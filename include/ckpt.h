@@ -722,8 +722,8 @@ typedef struct ckpt_gn_desc {
  * will do).  Calls that share one must not overlap.
  * Errors: CKPT_E_INVALID for sizes below 1, groups that do not divide c, an
  * unknown activation or type, a stride below c, eps <= 0; CKPT_E_UNSUPPORTED
- * for n hw c >= 2^35, n groups >= 2^25, or more than 1024 channels per group
- * (up to 4096 are served where 8 divides them). */
+ * for n hw c >= 2^35, n hw >= 2^30, n groups >= 2^25, c > 2^20, or more than
+ * 1024 channels per group (up to 4096 are served where 8 divides them). */
 int op_gn_workspace_bytes(const ckpt_gn_desc *desc, int32_t backward, uint64_t *bytes);
 
 /*

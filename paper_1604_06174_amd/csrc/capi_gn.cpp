@@ -84,16 +84,31 @@ ckpt::GnProblem problem_of(const ckpt_gn_desc *d, const std::string &fn) {
     const int64_t px = product(p.n, p.hw), e = px < 0 ? -1 : product(px, ld);
     if (e < 0 || e > (int64_t(1) << 60)) fail(CKPT_E_UNSUPPORTED, fn + ": tensor too large");
   }
+  if (p.C > (1 << 20)) fail(CKPT_E_UNSUPPORTED, fn + ": c must not exceed 2^20");
+  if (p.n * p.hw >= (int64_t(1) << 30)) fail(CKPT_E_UNSUPPORTED, fn + ": n*hw must stay below 2^30");
   if (p.n * p.hw * p.C >= kMaxElements) fail(CKPT_E_UNSUPPORTED, fn + ": n*hw*c must stay below 2^35");
   if (p.n * p.G >= (int64_t(1) << 25)) fail(CKPT_E_UNSUPPORTED, fn + ": n*groups must stay below 2^25");
   p.eps = d->eps;
   return p;
 }
 
-void grid_fits(const ckpt::GnPlan &g, const std::string &fn) {
-  // a launch counts its threads in 32 bits
-  if (g.blocks > (int64_t(1) << 32) / 1024 || g.lds > 65536)
-    fail(CKPT_E_UNSUPPORTED, fn + ": tensor too large");
+// block numbers the kernels divide (GnDivide)
+void grid_fits(const ckpt::GnCover &v, const std::string &fn) {
+  if (v.blocks >= (int64_t(1) << 21) || v.chunks >= (int64_t(1) << 21)) fail(CKPT_E_UNSUPPORTED, fn + ": tensor too large");
+}
+
+// a call's plan, its grids and workspace checked
+ckpt::GnPlan plan_of(const ckpt::GnProblem &p, bool backward, const void *workspace, uint64_t workspace_bytes,
+                     const std::string &fn) {
+  const ckpt::GnPlan g = ckpt::gn_plan(p, backward);
+  grid_fits(g.first, fn);
+  grid_fits(g.second, fn);
+  const uint64_t want = ckpt::gn_workspace_bytes(g);
+  if (want) {
+    need_ptr(workspace, fn + "(workspace)", 16);
+    if (workspace_bytes < want) fail(CKPT_E_WORKSPACE, fn + ": workspace smaller than op_gn_workspace_bytes");
+  }
+  return g;
 }
 
 }  // namespace
@@ -104,7 +119,7 @@ int op_gn_workspace_bytes(const ckpt_gn_desc *desc, int32_t backward, uint64_t *
   return ckpt::guarded([&] {
     need_ptr(bytes, "op_gn_workspace_bytes(bytes)");
     const ckpt::GnProblem p = problem_of(desc, "op_gn_workspace_bytes");
-    *bytes = ckpt::gn_workspace_bytes(p, backward != 0);
+    *bytes = ckpt::gn_workspace_bytes(ckpt::gn_plan(p, backward != 0));
   });
 }
 
@@ -120,14 +135,8 @@ int op_gn_forward(const ckpt_gn_desc *desc, const void *x, const float *gamma, c
     need_ptr(y, fn + "(y)", size_of(p.xf));
     need_ptr(st, fn + "(st)", 4);
     const ckpt::DropArgs da = drop_args(drop, fn);
-    grid_fits(ckpt::gn_plan(p, false), fn);
-    grid_fits(ckpt::gn_plan_elements(p), fn);
-    const uint64_t want = ckpt::gn_workspace_bytes(p, false);
-    if (want) {
-      need_ptr(workspace, fn + "(workspace)", 16);
-      if (workspace_bytes < want) fail(CKPT_E_WORKSPACE, fn + ": workspace smaller than op_gn_workspace_bytes");
-    }
-    ckpt::gn_forward(static_cast<hipStream_t>(stream), p, x, gamma, beta, da, y, st, workspace);
+    const ckpt::GnPlan plan = plan_of(p, false, workspace, workspace_bytes, fn);
+    ckpt::gn_forward(static_cast<hipStream_t>(stream), p, plan, x, gamma, beta, da, y, st, workspace);
     launched("op_gn_forward");
   });
 }
@@ -143,8 +152,9 @@ int op_gn_apply(const ckpt_gn_desc *desc, const void *x, const float *st, const 
     need_ptr(beta, fn + "(beta)", 4);
     need_ptr(y, fn + "(y)", size_of(p.xf));
     const ckpt::DropArgs da = drop_args(drop, fn);
-    grid_fits(ckpt::gn_plan_elements(p), fn);
-    ckpt::gn_apply(static_cast<hipStream_t>(stream), p, x, st, gamma, beta, da, y);
+    const ckpt::GnCover v = ckpt::gn_cover_rerun(p);
+    grid_fits(v, fn);
+    ckpt::gn_apply(static_cast<hipStream_t>(stream), p, v, x, st, gamma, beta, da, y);
     launched("op_gn_apply");
   });
 }
@@ -166,14 +176,8 @@ int op_gn_backward(const ckpt_gn_desc *desc, const void *g, const void *x, const
     need_ptr(dgamma, fn + "(dgamma)", 4);
     need_ptr(dbeta, fn + "(dbeta)", 4);
     const ckpt::DropArgs da = drop_args(drop, fn);
-    grid_fits(ckpt::gn_plan(p, true), fn);
-    grid_fits(ckpt::gn_plan_elements(p), fn);
-    const uint64_t want = ckpt::gn_workspace_bytes(p, true);
-    if (want) {
-      need_ptr(workspace, fn + "(workspace)", 16);
-      if (workspace_bytes < want) fail(CKPT_E_WORKSPACE, fn + ": workspace smaller than op_gn_workspace_bytes");
-    }
-    ckpt::gn_backward(static_cast<hipStream_t>(stream), p, g, x, st, gamma, beta, da, d, dgamma, dbeta, workspace);
+    const ckpt::GnPlan plan = plan_of(p, true, workspace, workspace_bytes, fn);
+    ckpt::gn_backward(static_cast<hipStream_t>(stream), p, plan, g, x, st, gamma, beta, da, d, dgamma, dbeta, workspace);
     launched("op_gn_backward");
   });
 }

@@ -1,0 +1,484 @@
+// Group norm with an activation and dropout, backward, over channels-last
+// tensors.  From x, the statistics, the counter and g alone (neither output nor
+// mask is kept):
+//
+//   t = x - mean, u = t a + beta (a = gamma rstd), xhat = t rstd
+//   du = dropout(g) act'(u), dbeta = sum du, dgamma = sum du xhat
+//   k1 = sum a du / m, k2 = rstd sum a du xhat / m over a group's m values
+//   d = a du - k1 - t k2
+//
+// As in the forward, a tile that fits stays in registers (x as loaded, du in
+// fp32): x and g are read once.  A larger one takes a pass for the channels'
+// sums per chunk of pixels and a second that adds up the chunks, folds the
+// channels into their groups and forms d.  Channel sums leave one record per
+// workgroup (or chunk), added in a fixed order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "gn.h"
+
+namespace ckpt {
+namespace gnb {
+
+// A vector column's parameters; du of one vector, in place of g.
+template <typename XT, int V, int NJ>
+struct Column {
+  float mean[NJ], a[V], beta[V];
+  template <bool SILU, bool DROP>
+  __device__ __forceinline__ void du(const GnArgs &A, const DropKey &key, const Vec<XT, V> &x, uint64_t pix, int c,
+                                     float g[V]) const {
+    if (DROP) gn_drop<V>(A, key, pix, c, g);
+    if (SILU || A.act == GN_ACT_RELU)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        g[j] = gn_act_bwd<SILU>(true, gn_affine(float(x.v[j]), mean[NJ == 1 ? 0 : j], a[j], beta[j]), g[j]);
+  }
+  template <typename DT>
+  __device__ __forceinline__ void put(const GnArgs &A, const Vec<XT, V> &x, const float (&k1)[NJ],
+                                      const float (&k2)[NJ], int64_t pix, int c, const float du[V]) const {
+    float v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int q = NJ == 1 ? 0 : j;
+      v[j] = a[j] * du[j] - k1[q] - (float(x.v[j]) - mean[q]) * k2[q];
+    }
+    store_vec<DT, V>(static_cast<DT *>(A.out) + pix * A.ldo + c, v);
+  }
+};
+
+// The channels' sums of a workgroup, ch[j] = sum du xhat and ch[V + j] = sum du of
+// a thread's pixels: record `by` of cpart, or dgamma and dbeta themselves.
+template <int V, bool WAVE, bool POW2>
+__device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE> &tm, int teams, int tile, int by,
+                                               float (&ch)[2 * V], float *lds) {
+  const int O = 2 * V * A.VC;
+  float *const out0 = A.cpart ? A.cpart + int64_t(by) * 2 * A.C : A.dgamma;
+  float *const out1 = A.cpart ? out0 + A.C : A.dbeta;
+  const float *sums = lds;
+  int parts, pitch;
+  if constexpr (POW2) {
+    const int w = threadIdx.x >> 6;
+    wave_columns<2 * V>(ch, threadIdx.x & 63, A.VC, tm.tx, lds + w * O);
+    parts = blockDim.x >> 6;
+    pitch = O;
+  } else {
+    const int tree = (A.TY + (A.TY + 7) / 8) * O;
+    float *const mine = lds + tm.index * tree;
+    if (tm.ty < A.TY)
+#pragma unroll
+      for (int k = 0; k < 2 * V; ++k) mine[tm.ty * O + k * A.VC + tm.tx] = ch[k];
+    sums = lds + (row_tree<WAVE, 2 * V>(tm, A.TY, A.VC, mine) - mine);
+    parts = teams;
+    pitch = tree;
+  }
+  __syncthreads();
+  // thread by channel, so that the record is written in order
+  for (int o = threadIdx.x; o < 2 * A.W; o += blockDim.x) {
+    const int q = o >= A.W, e = o - q * A.W, k = q * V + e % V;
+    float s = 0.f;
+    for (int r = 0; r < parts; ++r) s += sums[r * pitch + k * A.VC + e / V];
+    if (tile * A.W + e < A.C) (q ? out1 : out0)[tile * A.W + e] = s;
+  }
+}
+
+// Resident: one team per (sample, tile); a wavefront's loops over samples.
+template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, bool POW2, bool SILU,
+          bool DROP>
+__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4 ? 2 : 4) void k_gn_bwd(GnArgs A) {
+  extern __shared__ float lds[];
+  const Team<WAVE> tm(A);
+  const int teams = WAVE ? blockDim.x / 64 : 1;
+  const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles;
+  const int c = tile * A.W + tm.tx * V;
+  const bool col = c < A.C && tm.ty < A.TY;
+  float *const red = lds + tm.index * (POW2 ? 2 : 1) * A.redbuf;
+  int buf = 0;
+  const DropKey key = drop_key(A.drop);
+  const GnGroups<V, NJ> grp(A, col ? c : 0);
+  float ch[2 * V];
+#pragma unroll
+  for (int j = 0; j < 2 * V; ++j) ch[j] = 0.f;
+  for (int i = by * teams + tm.index; i < A.n; i = WAVE ? i + A.rows * teams : A.n) {
+    const int64_t pix0 = int64_t(i) * A.hw;
+    const XT *const x = static_cast<const XT *>(A.x) + (pix0 + tm.ty) * A.ldx + c;
+    const GT_ *const g = static_cast<const GT_ *>(A.g) + (pix0 + tm.ty) * A.ldg + c;
+    const int64_t dx = int64_t(A.TY) * A.ldx, dg = int64_t(A.TY) * A.ldg;
+    Vec<XT, V> xr[NV];
+    Vec<GT_, V> gr[NV];
+    float du[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (col && tm.ty + k * A.TY < A.hw) {
+        xr[k] = load_vec<XT, V>(x + k * dx);
+        gr[k] = load_vec<GT_, V>(g + k * dg);
+      }
+    Column<XT, V, NJ> cp;
+    float rstd[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      cp.mean[j] = A.st[i * A.G + grp.k[j]];
+      rstd[j] = A.st[(A.n + i) * A.G + grp.k[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      cp.a[j] = A.gamma[col ? c + j : j] * rstd[NJ == 1 ? 0 : j];
+      cp.beta[j] = A.beta[col ? c + j : j];
+    }
+    float s1[V], s2[V];  // sums of du and of du t
+#pragma unroll
+    for (int j = 0; j < V; ++j) s1[j] = s2[j] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (col && tm.ty + k * A.TY < A.hw) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) du[k][j] = float(gr[k].v[j]);
+        cp.template du<SILU, DROP>(A, key, xr[k], uint64_t(pix0 + tm.ty + k * A.TY), c, du[k]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          s1[j] += du[k][j];
+          s2[j] += du[k][j] * (float(xr[k].v[j]) - cp.mean[NJ == 1 ? 0 : j]);
+        }
+      }
+    float s[2 * NJ];
+#pragma unroll
+    for (int j = 0; j < 2 * NJ; ++j) s[j] = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int q = NJ == 1 ? 0 : j;
+      s2[j] *= rstd[q];
+      ch[j] += s2[j];
+      ch[V + j] += s1[j];
+      s[q] += cp.a[j] * s1[j];
+      s[NJ + q] += cp.a[j] * s2[j];
+    }
+    group_sums<2, NJ, V, WAVE, POW2>(A, tm, s, red + buf);
+    if (POW2) buf = A.redbuf - buf;
+    if (col) {
+      float k1[NJ], k2[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        k1[j] = s[j] * A.inv_m;
+        k2[j] = rstd[j] * s[NJ + j] * A.inv_m;
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (tm.ty + k * A.TY < A.hw) {
+          cp.template put<DT>(A, xr[k], k1, k2, pix0 + tm.ty + k * A.TY, c, du[k]);
+        }
+    }
+  }
+  __syncthreads();
+  channel_record<V, WAVE, POW2>(A, tm, teams, tile, by, ch, lds);
+}
+
+// The parameters of nc channels from c0 of sample i, in LDS: mean | a | beta, W each.
+__device__ __forceinline__ void channel_params(const GnArgs &A, int i, int c0, int nc, float *lds) {
+  for (int e = threadIdx.x; e < nc; e += blockDim.x) {
+    const int g = A.by_cg.of(c0 + e);
+    lds[e] = A.st[i * A.G + g];
+    lds[A.W + e] = A.gamma[c0 + e] * A.st[(A.n + i) * A.G + g];
+    lds[2 * A.W + e] = A.beta[c0 + e];
+  }
+}
+
+template <typename XT, int V>
+__device__ __forceinline__ void take_params(const GnArgs &A, int tx, const float *lds, Column<XT, V, V> &cp) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    cp.mean[j] = lds[tx * V + j];
+    cp.a[j] = lds[A.W + tx * V + j];
+    cp.beta[j] = lds[2 * A.W + tx * V + j];
+  }
+}
+
+// Split, first pass: a chunk's channel sums.
+template <typename XT, typename GT_, int V, bool POW2>
+__global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
+  extern __shared__ float lds[];
+  const Team<false> tm(A);
+  const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles, c0 = tile * A.W, c = c0 + tm.tx * V;
+  const int i = A.by_chunks.of(by), p0 = (by - i * A.chunks) * A.chunk, np = min(A.hw - p0, A.chunk);
+  const int64_t pix0 = int64_t(i) * A.hw + p0;
+  const bool col = c < A.C && tm.ty < A.TY;
+  const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
+  const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
+  constexpr int U = 2;
+  Vec<XT, V> xr[U];
+  Vec<GT_, V> gr[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (col && tm.ty + k * A.TY < np) {
+      xr[k] = load_vec<XT, V>(x + int64_t(tm.ty + k * A.TY) * A.ldx);
+      gr[k] = load_vec<GT_, V>(g + int64_t(tm.ty + k * A.TY) * A.ldg);
+    }
+  const DropKey key = drop_key(A.drop);
+  channel_params(A, i, c0, min(A.W, A.C - c0), lds);
+  __syncthreads();
+  float ch[2 * V];
+#pragma unroll
+  for (int j = 0; j < 2 * V; ++j) ch[j] = 0.f;
+  if (col) {
+    Column<XT, V, V> cp;
+    take_params(A, tm.tx, lds, cp);
+    gn_choose(A, [&](auto silu, auto drop) {
+      for (int r = tm.ty; r < np; r += U * A.TY) {
+        Vec<XT, V> nx[U];
+        Vec<GT_, V> ng[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+          if (r + (U + k) * A.TY < np) {
+            nx[k] = load_vec<XT, V>(x + int64_t(r + (U + k) * A.TY) * A.ldx);
+            ng[k] = load_vec<GT_, V>(g + int64_t(r + (U + k) * A.TY) * A.ldg);
+          }
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+          if (r + k * A.TY < np) {
+            float du[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) du[j] = float(gr[k].v[j]);
+            cp.template du<silu.value, drop.value>(A, key, xr[k], uint64_t(pix0 + r + k * A.TY), c, du);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              ch[j] += du[j] * (float(xr[k].v[j]) - cp.mean[j]);
+              ch[V + j] += du[j];
+            }
+          }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          xr[k] = nx[k];
+          gr[k] = ng[k];
+        }
+      }
+    });
+#pragma unroll
+    for (int j = 0; j < V; ++j) ch[j] *= A.st[(A.n + i) * A.G + A.by_cg.of(c + j)];
+  }
+  __syncthreads();
+  channel_record<V, false, POW2>(A, tm, 1, tile, by, ch, lds);
+}
+
+// dgamma | dbeta from `rows` records [2][C]: the 16 columns from 16 blk, a thread
+// per column and row in turn, added in a fixed order.  red: [blockDim / 16][17].
+__device__ __forceinline__ void record_sums(const GnArgs &A, int rows, int blk, float *red) {
+  const int e = blk * 16 + threadIdx.x % 16, r0 = threadIdx.x / 16, R = blockDim.x / 16;
+  float s = 0.f;
+  if (e < 2 * A.C) {
+    constexpr int U = 8;
+    for (int r = r0; r < rows; r += U * R) {
+      float v[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) v[k] = r + k * R < rows ? A.cpart[int64_t(r + k * R) * 2 * A.C + e] : 0.f;
+#pragma unroll
+      for (int k = 0; k < U; ++k) s += v[k];
+    }
+  }
+  red[r0 * 17 + threadIdx.x % 16] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && e < 2 * A.C) {
+    s = 0.f;
+    for (int r = 0; r < R; ++r) s += red[r * 17 + threadIdx.x];
+    (e < A.C ? A.dgamma : A.dbeta)[e < A.C ? e : e - A.C] = s;
+  }
+}
+
+// Split, second pass: d of a chunk of one sample's pixels.  The first `sums`
+// workgroups add up the records of dgamma and dbeta beside it.  MERGED: the
+// groups' sums are in gsum; else the tile holds whole groups and forms them from
+// the chunks' channel sums.
+template <typename XT, typename GT_, typename DT, int V, bool MERGED>
+__global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, int sums) {
+  extern __shared__ float lds[];
+  if (int(blockIdx.x) < sums) return record_sums(A, A.n * A.chunks1, blockIdx.x, lds);
+  const int t = threadIdx.x, T = blockDim.x, ty = A.by_vc.of(t), tx = t - ty * A.VC;
+  const int blk = blockIdx.x - sums, by = A.by_tiles.of(blk), c0 = (blk - by * A.tiles) * A.W, c = c0 + tx * V;
+  const int i = A.by_chunks.of(by), p0 = (by - i * A.chunks) * A.chunk, np = min(A.hw - p0, A.chunk);
+  const int64_t pix0 = int64_t(i) * A.hw + p0;
+  const bool col = c < A.C && ty < A.TY;
+  const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
+  const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
+  constexpr int U = 2;
+  Vec<XT, V> xr[U];
+  Vec<GT_, V> gr[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (col && ty + k * A.TY < np) {
+      xr[k] = load_vec<XT, V>(x + int64_t(ty + k * A.TY) * A.ldx);
+      gr[k] = load_vec<GT_, V>(g + int64_t(ty + k * A.TY) * A.ldg);
+    }
+  const DropKey key = drop_key(A.drop);
+  const int nc = min(A.W, A.C - c0);
+  channel_params(A, i, c0, nc, lds);
+  float *const kk = lds + 3 * A.W;  // k1 | k2, W each
+  if (MERGED) {
+    for (int e = t; e < nc; e += T) {
+      const int k = i * A.G + A.by_cg.of(c0 + e);
+      kk[e] = A.gsum[2 * k] * A.inv_m;
+      kk[A.W + e] = A.st[A.n * A.G + k] * A.gsum[2 * k + 1] * A.inv_m;
+    }
+    __syncthreads();
+  } else {
+    // the tile's channel sums, du xhat then du: the chunks dealt to T / (2 W) threads each
+    float *const part = kk + 2 * A.W;
+    const int S = max(1, T / (2 * A.W));
+    for (int o = t; o < 2 * A.W * S; o += T) {
+      const int e = o % (2 * A.W), q = e >= A.W, cc = c0 + e - q * A.W;
+      float s = 0.f;
+      if (cc < A.C) {
+        const float *const r = A.cpart + int64_t(i) * A.chunks1 * 2 * A.C + q * A.C + cc;
+        constexpr int P = 8;
+        for (int k = o / (2 * A.W); k < A.chunks1; k += P * S) {
+          float v[P];
+#pragma unroll
+          for (int u = 0; u < P; ++u) v[u] = k + u * S < A.chunks1 ? r[int64_t(k + u * S) * 2 * A.C] : 0.f;
+#pragma unroll
+          for (int u = 0; u < P; ++u) s += v[u];
+        }
+      }
+      part[o] = s;
+    }
+    __syncthreads();
+    for (int e = t; e < 2 * A.W; e += T) {
+      float s = 0.f;
+      for (int k = 0; k < S; ++k) s += part[k * 2 * A.W + e];
+      part[e] = s * lds[A.W + e % A.W];  // times a; only this thread reads what it overwrites
+    }
+    __syncthreads();
+    for (int e = t; e < nc; e += T) {
+      const int f = A.by_cg.of(e) * A.cg;
+      float s1 = 0.f, s2 = 0.f;
+      for (int k = 0; k < A.cg; ++k) {
+        s2 += part[f + k];
+        s1 += part[A.W + f + k];
+      }
+      kk[e] = s1 * A.inv_m;
+      kk[A.W + e] = A.st[(A.n + i) * A.G + A.by_cg.of(c0 + e)] * s2 * A.inv_m;
+    }
+    __syncthreads();
+  }
+  if (!col) return;
+  Column<XT, V, V> cp;
+  take_params(A, tx, lds, cp);
+  float k1[V], k2[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    k1[j] = kk[tx * V + j];
+    k2[j] = kk[A.W + tx * V + j];
+  }
+  gn_choose(A, [&](auto silu, auto drop) {
+    for (int r = ty; r < np; r += U * A.TY) {
+      Vec<XT, V> nx[U];
+      Vec<GT_, V> ng[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (r + (U + k) * A.TY < np) {
+          nx[k] = load_vec<XT, V>(x + int64_t(r + (U + k) * A.TY) * A.ldx);
+          ng[k] = load_vec<GT_, V>(g + int64_t(r + (U + k) * A.TY) * A.ldg);
+        }
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (r + k * A.TY < np) {
+          float du[V];
+#pragma unroll
+          for (int j = 0; j < V; ++j) du[j] = float(gr[k].v[j]);
+          cp.template du<silu.value, drop.value>(A, key, xr[k], uint64_t(pix0 + r + k * A.TY), c, du);
+          cp.template put<DT>(A, xr[k], k1, k2, pix0 + r + k * A.TY, c, du);
+        }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        xr[k] = nx[k];
+        gr[k] = ng[k];
+      }
+    }
+  });
+}
+
+// many chunks or wide groups: gsum[i][k] = sum a du | sum a du xhat of one group
+void merge_groups(hipStream_t s, const GnArgs &a);
+// dgamma | dbeta from the resident passes' records
+void sum_records(hipStream_t s, const GnArgs &a);
+
+template <typename XT, typename GT_, typename DT, int V, int NV, int NJ>
+void launch_resident(hipStream_t s, const GnPlan &g, const GnArgs &a) {
+  const dim3 grid(uint32_t(g.first.blocks)), block(g.first.threads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, g.lds, s, a); };
+  gn_choose(a, [&](auto silu, auto drop) {
+    constexpr bool S = decltype(silu)::value, D = decltype(drop)::value;
+    // a wavefront's tile ends at 8 vectors a thread (gn_plan)
+    if constexpr (NV <= 8)
+      if (g.wave)
+        return g.pow2 ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, true, S, D>)
+                      : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, false, S, D>);
+    g.pow2 ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, true, S, D>)
+           : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, false, S, D>);
+  });
+}
+
+template <typename XT, typename GT_, typename DT, int V, int NJ>
+void run(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {
+  if (g.resident) {
+    if (V == 8 && g.NV <= 1)
+      launch_resident<XT, GT_, DT, V, 1, NJ>(s, g, a);
+    else if (V == 8 && g.NV <= 2)
+      launch_resident<XT, GT_, DT, V, 2, NJ>(s, g, a);
+    else if (g.NV <= 4)
+      launch_resident<XT, GT_, DT, V, 4, NJ>(s, g, a);
+    else if (g.NV <= 8)
+      launch_resident<XT, GT_, DT, V, 8, NJ>(s, g, a);
+    else if constexpr (V == 1)  // vectors stop at 8 (gn_plan)
+      launch_resident<XT, GT_, DT, V, 16, NJ>(s, g, a);
+    if (g.rows > 1) sum_records(s, a);
+    return;
+  }
+  const GnCover &v = g.first, &w = g.second;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(uint32_t(v.blocks)), dim3(v.threads), std::max(g.lds, size_t(12) * v.W), s, a);
+  };
+  g.pow2 ? go(k_gn_bwd_sums<XT, GT_, V, true>) : go(k_gn_bwd_sums<XT, GT_, V, false>);
+  GnArgs b = gn_args(p, w, a.drop);
+  b.x = a.x;
+  b.g = a.g;
+  b.out = a.out;
+  b.ldo = a.ldo;
+  b.gamma = a.gamma;
+  b.beta = a.beta;
+  b.st = a.st;
+  b.cpart = a.cpart;
+  b.gsum = a.gsum;
+  b.dgamma = a.dgamma;
+  b.dbeta = a.dbeta;
+  b.chunks1 = int(v.chunks);
+  b.chunk1 = int(v.chunk);
+  const int sums = (2 * p.C + 15) / 16;
+  const dim3 grid(uint32_t(w.blocks + sums)), block(w.threads);
+  const size_t red = size_t(w.threads / 16) * 17;
+  const size_t params = 5 * size_t(w.W);
+  if (g.merge) {
+    merge_groups(s, b);
+    hipLaunchKernelGGL((k_gn_bwd_apply<XT, GT_, DT, V, true>), grid, block, 4 * std::max(red, params), s, b, sums);
+  } else {
+    const size_t part = 2 * size_t(w.W) * std::max(1, w.threads / (2 * w.W));
+    hipLaunchKernelGGL((k_gn_bwd_apply<XT, GT_, DT, V, false>), grid, block, 4 * std::max(red, params + part), s, b,
+                       sums);
+  }
+}
+
+template <typename XT, typename GT_, typename DT>
+void run_types(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {
+  if (g.first.V == 1)
+    run<XT, GT_, DT, 1, 1>(s, p, g, a);
+  else if (g.NJ == 1)
+    run<XT, GT_, DT, 8, 1>(s, p, g, a);
+  else
+    run<XT, GT_, DT, 8, 8>(s, p, g, a);
+}
+
+void run_f32(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a);
+void run_bf16_f32(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a);
+void run_bf16_bf16(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a);
+
+}  // namespace gnb
+}  // namespace ckpt

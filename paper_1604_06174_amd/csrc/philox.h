@@ -44,9 +44,9 @@ __device__ __forceinline__ void philox(const DropKey &k, uint32_t blk, uint32_t 
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = uint64_t(c0) * 0xD2511F53u, b = uint64_t(c2) * 0xCD9E8D57u;
-    c0 = uint32_t(b >> 32) ^ c1 ^ k0;
+    c0 = __builtin_amdgcn_bitop3_b32(uint32_t(b >> 32), c1, k0, 0x96);  // the three's exclusive or
     c1 = uint32_t(b);
-    c2 = uint32_t(a >> 32) ^ c3 ^ k1;
+    c2 = __builtin_amdgcn_bitop3_b32(uint32_t(a >> 32), c3, k1, 0x96);
     c3 = uint32_t(a);
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
