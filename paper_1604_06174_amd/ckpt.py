@@ -648,12 +648,15 @@ def op_maxpool(backward, n, h, w, c, ho, wo, r, out, g=None, y=None, arg=None, s
 
 
 # ------------------------------------------------- group norm and dropout --
+_TYPE_CODES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+
+
 def type_of(t) -> int:
     """The type code of a torch tensor."""
-    codes = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
-    if t.dtype not in codes:
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
         raise CkptError(E_UNSUPPORTED, f"tensors are float32 or bfloat16, not {t.dtype}")
-    return codes[t.dtype]
+    return code
 
 
 def dropout(rng, p: float, site: int = 0) -> Dropout:
@@ -671,33 +674,29 @@ def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=N
                   ldx, ldy, ldg, ldd, eps, 0)
 
 
-def _byref(x):
-    return None if x is None else C.byref(x)
-
-
 def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
     v = C.c_uint64()
-    _check(_lib.op_gn_workspace_bytes(_byref(desc), int(backward), C.byref(v)))
+    _check(_lib.op_gn_workspace_bytes(desc, int(backward), C.byref(v)))
     return v.value
 
 
 def op_gn_forward(desc, x, gamma, beta, y, st, workspace=None, workspace_bytes=0, drop=None, stream=None):
-    _check(_lib.op_gn_forward(_byref(desc), _addr(x), _addr(gamma), _addr(beta), _byref(drop), _addr(y), _addr(st),
+    _check(_lib.op_gn_forward(desc, _addr(x), _addr(gamma), _addr(beta), drop, _addr(y), _addr(st),
                               _addr(workspace), int(workspace_bytes), _s(stream)))
 
 
 def op_gn_apply(desc, x, st, gamma, beta, y, drop=None, stream=None):
-    _check(_lib.op_gn_apply(_byref(desc), _addr(x), _addr(st), _addr(gamma), _addr(beta), _byref(drop), _addr(y),
+    _check(_lib.op_gn_apply(desc, _addr(x), _addr(st), _addr(gamma), _addr(beta), drop, _addr(y),
                             _s(stream)))
 
 
 def op_gn_backward(desc, g, x, st, gamma, beta, d, dgamma, dbeta, workspace=None, workspace_bytes=0, drop=None,
                    stream=None):
-    _check(_lib.op_gn_backward(_byref(desc), _addr(g), _addr(x), _addr(st), _addr(gamma), _addr(beta), _byref(drop),
+    _check(_lib.op_gn_backward(desc, _addr(g), _addr(x), _addr(st), _addr(gamma), _addr(beta), drop,
                                _addr(d), _addr(dgamma), _addr(dbeta), _addr(workspace), int(workspace_bytes),
                                _s(stream)))
 
 
 def op_dropout(rows, cols, x, y, drop, res=None, xtype=TYPE_BF16, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
     _check(_lib.op_dropout(rows, cols, xtype, _addr(x), ldx, _addr(res), ldr, xtype if ytype is None else ytype,
-                           _addr(y), ldy, _byref(drop), _s(stream)))
+                           _addr(y), ldy, drop, _s(stream)))

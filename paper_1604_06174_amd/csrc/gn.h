@@ -29,12 +29,18 @@ struct GnProblem {
 };
 
 // How a pass covers it.  A tile is W consecutive channels (whole vectors of V) of
-// one sample: VC = W / V threads cover a pixel, TY pixels are covered at once.
+// one sample: VC threads cover a pixel (cols = W / V of them with a vector; the rest,
+// where VC is rounded up to a power of two, idle), TY pixels are covered at once.
 struct GnCover {
-  int V, W, tiles, VC, TY, threads;
+  int V, W, tiles, cols, VC, TY, threads;
   int64_t chunks, chunk;  // a sample's pixels: chunks of `chunk`
   int64_t blocks;
 };
+
+// How a team's sums are reduced: in LDS alone (VC above 64); within wavefronts first
+// (VC a power of two, at most 64); and that with whole groups filling the columns, so
+// that a group of vectors is a power of two of them (VC = cols).
+enum { GN_RED_TREE = 0, GN_RED_COLUMNS = 1, GN_RED_GROUPS = 2 };
 
 // The passes of a call.
 struct GnPlan {
@@ -43,12 +49,13 @@ struct GnPlan {
   // workgroup is the team, its samples' `rows` records of channel sums)
   bool resident, wave;
   int NV, teams;
+  int pack;  // samples of one pixel that a wavefront takes at once (1: its rows are pixels)
   int64_t rows;
   // split: `first` leaves every chunk's sums, `second` applies them, adding them up by
   // itself (`merge`: a launch between them does)
   bool merge;
   int NJ;      // values a vector's sums consist of: 1 (it lies within one group) or V
-  bool pow2;   // VC is a power of two, at most 64: wavefronts reduce in registers
+  int red;     // how sums are reduced: GN_RED_*
   int redbuf;  // floats of LDS of one reduction
   size_t lds;
   GnCover first, second;  // resident: `first` alone
@@ -97,8 +104,8 @@ struct GnArgs {
   GnDivide by_tiles, by_chunks, by_vc, by_cg;
   int64_t ldx, ldg, ldo;
   float eps, inv_m;
-  int W, tiles, VC, TY;
-  int redbuf;
+  int W, tiles, cols, VC, TY;
+  int redbuf, pack;
   DropArgs drop;
 };
 
@@ -123,6 +130,7 @@ inline GnArgs gn_args(const GnProblem &p, const GnCover &v, const DropArgs &drop
   a.inv_m = float(1.0 / (double(p.hw) * p.cg));
   a.W = v.W;
   a.tiles = v.tiles;
+  a.cols = v.cols;
   a.VC = v.VC;
   a.TY = v.TY;
   a.drop = drop;
@@ -157,9 +165,10 @@ struct Team {
 };
 
 // floats of LDS one call of group_sums<NQ, NJ> uses per team of T threads
-inline int gn_reduce_floats(const GnCover &v, bool pow2, int T, int NQ, int NJ, int cg) {
+inline int gn_reduce_floats(const GnCover &v, int red, int T, int NQ, int NJ, int cg) {
   const int gt = NQ * (v.W / cg);
-  if (pow2) return T / 64 * NQ * (NJ == 1 ? gt / NQ : v.VC * NJ) + gt;
+  if (red == GN_RED_GROUPS && NJ == 1) return T / 64 * gt;
+  if (red != GN_RED_TREE) return (T > 64 ? T / 64 + 1 : 1) * NQ * v.VC * NJ + gt;
   return (v.TY + (v.TY + 7) / 8) * v.VC * NQ * NJ + gt;
 }
 
@@ -192,88 +201,127 @@ __device__ __forceinline__ float *row_tree(const Team<WAVE> &tm, int TY, int VC,
   return src;
 }
 
+// The sum of n values `pitch` apart, the reads of four at a time in flight.
+__device__ __forceinline__ float strided_sum(const float *p, int n, int pitch) {
+  float s = 0.f;
+  for (int i = 0; i < n; i += 4) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = p[min(i + u, n - 1) * pitch];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s += i + u < n ? v[u] : 0.f;
+  }
+  return s;
+}
+
+// Sums over whole groups, VC a power of two: quantity q of the m-th of M groups in a
+// vector at val[q M + m], or (M = 1) of a group of q1 vectors.  g0: the group (of the
+// tile's GT) of the thread's first value; `first`: its vector is that group's first.
+template <int NQ, int M, bool WAVE>
+__device__ __forceinline__ void whole_groups(const GnArgs &a, const Team<WAVE> &tm, float (&val)[NQ * M], int q1,
+                                             int g0, bool first, int GT, float *red) {
+  const int lane = tm.t & 63, w = tm.t >> 6, nw = tm.T / 64;
+  add_from<NQ * M>(WAVE && a.pack > 1 ? 64 : a.VC, val);  // packed: every row is a sample
+  if (M == 1) add_below<NQ * M>(q1, val);
+  if (nw == 1) return;
+  if (lane < a.VC && first)
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int m = 0; m < M; ++m) red[(w * NQ + q) * GT + g0 + m] = val[q * M + m];
+  tm.sync();
+#pragma unroll
+  for (int q = 0; q < NQ; ++q)
+#pragma unroll
+    for (int m = 0; m < M; ++m) val[q * M + m] = strided_sum(red + q * GT + g0 + m, nw, NQ * GT);
+}
+
 // val[q NJ + j], q < NQ: quantity q of the thread's pixels, of its vector (NJ = 1,
-// the vector lies within one group) or of its channel j (NJ = V).  Replaced by the sum over the whole group it belongs to.
-// POW2: VC is a power of two, at most 64.  red: redbuf floats of LDS, POW2: another
-// ones than the call before's.
-template <int NQ, int NJ, int V, bool WAVE, bool POW2>
+// the vector lies within one group) or of its channel j (NJ = V).  Replaced by the
+// sum over the whole group it belongs to.  red: redbuf floats of LDS, where RED is
+// GN_RED_GROUPS other ones than the call before's (one barrier may be all there is
+// between a call's reads and the next one's writes; the others have two).
+template <int NQ, int NJ, int V, bool WAVE, int RED>
 __device__ __forceinline__ void group_sums(const GnArgs &a, const Team<WAVE> &tm, float (&val)[NQ * NJ],
                                            float *red) {
   constexpr int NVAL = NQ * NJ;
   const int GT = a.by_cg.of(a.W);            // groups of the tile
   const int q1 = NJ == 1 ? a.cg / V : a.cg;  // values of a group
   const int lane = tm.t & 63, w = tm.t >> 6, nw = tm.T / 64;
-  if constexpr (POW2 && NJ == 1) {
-    add_from<NVAL>(a.VC, val);
-    add_below<NVAL>(q1, val);  // VC = GT q1 is a power of two, so q1 is one
-    if (nw == 1) return;
+  if constexpr (RED == GN_RED_GROUPS && NJ == 1) {
+    // VC = GT q1 is a power of two, so q1 is one
     const int grp = a.by_cg.of(tm.tx * V);
-    if (lane < a.VC && grp * a.cg == tm.tx * V)
-#pragma unroll
-      for (int k = 0; k < NVAL; ++k) red[(w * NQ + k) * GT + grp] = val[k];
-    tm.sync();
-#pragma unroll
-    for (int k = 0; k < NVAL; ++k) {
-      // the reads of four wavefronts' sums at a time in flight
-      float s = 0.f;
-      for (int i = 0; i < nw; i += 4) {
-        float v[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = red[(min(i + u, nw - 1) * NQ + k) * GT + grp];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) s += i + u < nw ? v[u] : 0.f;
-      }
-      val[k] = s;
-    }
+    whole_groups<NQ, 1, WAVE>(a, tm, val, q1, grp, grp * a.cg == tm.tx * V, GT, red);
     return;
   }
+  if constexpr (RED == GN_RED_GROUPS && NJ == 8) {
+    // groups of two or four channels: several whole ones in a vector
+    auto fold = [&](auto cg) {
+      constexpr int CG = decltype(cg)::value, M = NJ / CG;
+      float v[NQ * M];
+#pragma unroll
+      for (int k = 0; k < NQ * M; ++k) {
+        v[k] = val[k * CG];
+#pragma unroll
+        for (int j = 1; j < CG; ++j) v[k] += val[k * CG + j];
+      }
+      whole_groups<NQ, M, WAVE>(a, tm, v, 1, tm.tx * M, true, GT, red);
+#pragma unroll
+      for (int k = 0; k < NVAL; ++k) val[k] = v[k / CG];
+    };
+    if (a.cg == 2) return fold(std::integral_constant<int, 2>());
+    if (a.cg == 4) return fold(std::integral_constant<int, 4>());
+  }
   const int O = a.VC * NVAL;
-  const float *col;  // `parts` records of the columns' sums, value k of column tx at k VC + tx
+  float *col;  // the columns' sums, value k of column tx at k VC + tx
   float *gt;
-  int parts;
-  if constexpr (POW2) {
+  if constexpr (RED != GN_RED_TREE) {
     wave_columns<NVAL>(val, lane, a.VC, tm.tx, red + w * O);
     tm.sync();
     col = red;
-    parts = nw;
-    gt = red + nw * O;
+    gt = red + O;
+    if (nw > 1) {
+      gt = red + (nw + 1) * O;
+      col = red + nw * O;
+      for (int o = tm.t; o < O; o += tm.T) col[o] = strided_sum(red + o, nw, O);
+      tm.sync();
+    }
   } else {
     tm.sync();
     if (tm.ty < a.TY)
 #pragma unroll
       for (int k = 0; k < NVAL; ++k) red[tm.ty * O + k * a.VC + tm.tx] = val[k];
     col = row_tree<WAVE, NVAL>(tm, a.TY, a.VC, red);
-    parts = 1;
     gt = red + (a.TY + (a.TY + 7) / 8) * O;
   }
   // value i of the tile, of quantity q
-  auto at = [&](int q, int i) {
-    const int k = (q * NJ + i % NJ) * a.VC + i / NJ;
-    float s = 0.f;
-    for (int r = 0; r < parts; ++r) s += col[r * O + k];
-    return s;
-  };
+  auto at = [&](int q, int i) { return col[(q * NJ + i % NJ) * a.VC + i / NJ]; };
   if (q1 <= 16) {
     for (int g = tm.t; g < GT * NQ; g += tm.T) {
       const int q = NQ == 2 && g >= GT, i0 = (g - q * GT) * q1;
       float s = 0.f;
-      for (int i = 0; i < q1; ++i) s += at(q, i0 + i);
+      for (int i = 0; i < q1; i += 4) {
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = at(q, i0 + min(i + u, q1 - 1));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s += i + u < q1 ? v[u] : 0.f;
+      }
       gt[g] = s;
     }
   } else {
     for (int g = w; g < GT * NQ; g += nw) {
       const int q = NQ == 2 && g >= GT, i0 = (g - q * GT) * q1;
-      float s = 0.f;
-      for (int i = lane; i < q1; i += 64) s += at(q, i0 + i);
-      float all[1] = {s};
-      add_from<1>(1, all);
-      if (lane == 0) gt[g] = all[0];
+      float s[1] = {0.f};
+      for (int i = lane; i < q1; i += 64) s[0] += at(q, i0 + i);
+      add_from<1>(1, s);
+      if (lane == 0) gt[g] = s[0];
     }
   }
   tm.sync();
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int grp = a.by_cg.of(tm.tx * V + j);
+    const int grp = min(a.by_cg.of(tm.tx * V + j), GT - 1);  // an idle column's is nobody's
 #pragma unroll
     for (int q = 0; q < NQ; ++q) val[q * NJ + j] = gt[q * GT + grp];
   }

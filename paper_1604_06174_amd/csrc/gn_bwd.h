@@ -52,7 +52,7 @@ struct Column {
 
 // The channels' sums of a workgroup, ch[j] = sum du xhat and ch[V + j] = sum du of
 // a thread's pixels: record `by` of cpart, or dgamma and dbeta themselves.
-template <int V, bool WAVE, bool POW2>
+template <int V, bool WAVE, int RED>
 __device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE> &tm, int teams, int tile, int by,
                                                float (&ch)[2 * V], float *lds) {
   const int O = 2 * V * A.VC;
@@ -60,7 +60,7 @@ __device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE>
   float *const out1 = A.cpart ? out0 + A.C : A.dbeta;
   const float *sums = lds;
   int parts, pitch;
-  if constexpr (POW2) {
+  if constexpr (RED != GN_RED_TREE) {
     const int w = threadIdx.x >> 6;
     wave_columns<2 * V>(ch, threadIdx.x & 63, A.VC, tm.tx, lds + w * O);
     parts = blockDim.x >> 6;
@@ -86,7 +86,7 @@ __device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE>
 }
 
 // Resident: one team per (sample, tile); a wavefront's loops over samples.
-template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, bool POW2, bool SILU,
+template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, int RED, bool SILU,
           bool DROP>
 __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4 ? 2 : 4) void k_gn_bwd(GnArgs A) {
   extern __shared__ float lds[];
@@ -94,25 +94,30 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4
   const int teams = WAVE ? blockDim.x / 64 : 1;
   const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles;
   const int c = tile * A.W + tm.tx * V;
-  const bool col = c < A.C && tm.ty < A.TY;
-  float *const red = lds + tm.index * (POW2 ? 2 : 1) * A.redbuf;
+  const bool column = tm.tx < A.cols && c < A.C;
+  float *const red = lds + tm.index * (RED == GN_RED_GROUPS ? 2 : 1) * A.redbuf;
   int buf = 0;
   const DropKey key = drop_key(A.drop);
-  const GnGroups<V, NJ> grp(A, col ? c : 0);
+  const GnGroups<V, NJ> grp(A, column ? c : 0);
   float ch[2 * V];
 #pragma unroll
   for (int j = 0; j < 2 * V; ++j) ch[j] = 0.f;
-  for (int i = by * teams + tm.index; i < A.n; i = WAVE ? i + A.rows * teams : A.n) {
+  // a wavefront's rows are pixels, or samples of one
+  const bool packed = WAVE && A.pack > 1;
+  const int ty = packed ? 0 : tm.ty, step = A.rows * teams * (WAVE ? A.pack : 1);
+  for (int i0 = (by * teams + tm.index) * (WAVE ? A.pack : 1); i0 < A.n; i0 = WAVE ? i0 + step : A.n) {
+    const bool live = !packed || i0 + tm.ty < A.n, col = column && live && ty < A.TY;
+    const int i = packed ? min(i0 + tm.ty, A.n - 1) : i0;
     const int64_t pix0 = int64_t(i) * A.hw;
-    const XT *const x = static_cast<const XT *>(A.x) + (pix0 + tm.ty) * A.ldx + c;
-    const GT_ *const g = static_cast<const GT_ *>(A.g) + (pix0 + tm.ty) * A.ldg + c;
+    const XT *const x = static_cast<const XT *>(A.x) + (pix0 + ty) * A.ldx + c;
+    const GT_ *const g = static_cast<const GT_ *>(A.g) + (pix0 + ty) * A.ldg + c;
     const int64_t dx = int64_t(A.TY) * A.ldx, dg = int64_t(A.TY) * A.ldg;
     Vec<XT, V> xr[NV];
     Vec<GT_, V> gr[NV];
     float du[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (col && tm.ty + k * A.TY < A.hw) {
+      if (col && ty + k * A.TY < A.hw) {
         xr[k] = load_vec<XT, V>(x + k * dx);
         gr[k] = load_vec<GT_, V>(g + k * dg);
       }
@@ -133,10 +138,10 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4
     for (int j = 0; j < V; ++j) s1[j] = s2[j] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (col && tm.ty + k * A.TY < A.hw) {
+      if (col && ty + k * A.TY < A.hw) {
 #pragma unroll
         for (int j = 0; j < V; ++j) du[k][j] = float(gr[k].v[j]);
-        cp.template du<SILU, DROP>(A, key, xr[k], uint64_t(pix0 + tm.ty + k * A.TY), c, du[k]);
+        cp.template du<SILU, DROP>(A, key, xr[k], uint64_t(pix0 + ty + k * A.TY), c, du[k]);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           s1[j] += du[k][j];
@@ -155,8 +160,8 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4
       s[q] += cp.a[j] * s1[j];
       s[NJ + q] += cp.a[j] * s2[j];
     }
-    group_sums<2, NJ, V, WAVE, POW2>(A, tm, s, red + buf);
-    if (POW2) buf = A.redbuf - buf;
+    group_sums<2, NJ, V, WAVE, RED>(A, tm, s, red + buf);
+    if (RED == GN_RED_GROUPS) buf = A.redbuf - buf;
     if (col) {
       float k1[NJ], k2[NJ];
 #pragma unroll
@@ -166,13 +171,13 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (tm.ty + k * A.TY < A.hw) {
-          cp.template put<DT>(A, xr[k], k1, k2, pix0 + tm.ty + k * A.TY, c, du[k]);
+        if (ty + k * A.TY < A.hw) {
+          cp.template put<DT>(A, xr[k], k1, k2, pix0 + ty + k * A.TY, c, du[k]);
         }
     }
   }
   __syncthreads();
-  channel_record<V, WAVE, POW2>(A, tm, teams, tile, by, ch, lds);
+  channel_record<V, WAVE, RED>(A, tm, teams, tile, by, ch, lds);
 }
 
 // The parameters of nc channels from c0 of sample i, in LDS: mean | a | beta, W each.
@@ -196,17 +201,17 @@ __device__ __forceinline__ void take_params(const GnArgs &A, int tx, const float
 }
 
 // Split, first pass: a chunk's channel sums.
-template <typename XT, typename GT_, int V, bool POW2>
+template <typename XT, typename GT_, int V, int RED>
 __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
   extern __shared__ float lds[];
   const Team<false> tm(A);
   const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles, c0 = tile * A.W, c = c0 + tm.tx * V;
   const int i = A.by_chunks.of(by), p0 = (by - i * A.chunks) * A.chunk, np = min(A.hw - p0, A.chunk);
   const int64_t pix0 = int64_t(i) * A.hw + p0;
-  const bool col = c < A.C && tm.ty < A.TY;
+  const bool col = tm.tx < A.cols && c < A.C && tm.ty < A.TY;
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
   const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
-  constexpr int U = 2;
+  constexpr int U = 1;
   Vec<XT, V> xr[U];
   Vec<GT_, V> gr[U];
 #pragma unroll
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
     for (int j = 0; j < V; ++j) ch[j] *= A.st[(A.n + i) * A.G + A.by_cg.of(c + j)];
   }
   __syncthreads();
-  channel_record<V, false, POW2>(A, tm, 1, tile, by, ch, lds);
+  channel_record<V, false, RED>(A, tm, 1, tile, by, ch, lds);
 }
 
 // dgamma | dbeta from `rows` records [2][C]: the 16 columns from 16 blk, a thread
@@ -300,7 +305,7 @@ __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, 
   const bool col = c < A.C && ty < A.TY;
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
   const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
-  constexpr int U = 2;
+  constexpr int U = 1;
   Vec<XT, V> xr[U];
   Vec<GT_, V> gr[U];
 #pragma unroll
@@ -407,22 +412,23 @@ void launch_resident(hipStream_t s, const GnPlan &g, const GnArgs &a) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, g.lds, s, a); };
   gn_choose(a, [&](auto silu, auto drop) {
     constexpr bool S = decltype(silu)::value, D = decltype(drop)::value;
-    // a wavefront's tile ends at 8 vectors a thread (gn_plan)
-    if constexpr (NV <= 8)
+    // a wavefront's tile ends at two vectors a thread (gn_plan)
+    if constexpr (NV <= 2)
       if (g.wave)
-        return g.pow2 ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, true, S, D>)
-                      : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, false, S, D>);
-    g.pow2 ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, true, S, D>)
-           : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, false, S, D>);
+        return g.red == GN_RED_GROUPS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, GN_RED_GROUPS, S, D>)
+                                      : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, GN_RED_COLUMNS, S, D>);
+    g.red == GN_RED_GROUPS    ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_GROUPS, S, D>)
+    : g.red == GN_RED_COLUMNS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_COLUMNS, S, D>)
+                              : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_TREE, S, D>);
   });
 }
 
 template <typename XT, typename GT_, typename DT, int V, int NJ>
 void run(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {
   if (g.resident) {
-    if (V == 8 && g.NV <= 1)
+    if (g.NV <= 1)
       launch_resident<XT, GT_, DT, V, 1, NJ>(s, g, a);
-    else if (V == 8 && g.NV <= 2)
+    else if (g.NV <= 2)
       launch_resident<XT, GT_, DT, V, 2, NJ>(s, g, a);
     else if (g.NV <= 4)
       launch_resident<XT, GT_, DT, V, 4, NJ>(s, g, a);
@@ -437,7 +443,7 @@ void run(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(uint32_t(v.blocks)), dim3(v.threads), std::max(g.lds, size_t(12) * v.W), s, a);
   };
-  g.pow2 ? go(k_gn_bwd_sums<XT, GT_, V, true>) : go(k_gn_bwd_sums<XT, GT_, V, false>);
+  g.red == GN_RED_TREE ? go(k_gn_bwd_sums<XT, GT_, V, GN_RED_TREE>) : go(k_gn_bwd_sums<XT, GT_, V, GN_RED_COLUMNS>);
   GnArgs b = gn_args(p, w, a.drop);
   b.x = a.x;
   b.g = a.g;

@@ -5,24 +5,48 @@ namespace ckpt {
 namespace gnb {
 namespace {
 
-__global__ __launch_bounds__(64) void k_gn_bwd_merge(GnArgs A) {
-  const int i = blockIdx.x / A.G, k = blockIdx.x % A.G;
+// One workgroup per group of a sample: its channels across the threads, eight chunks
+// at a time in flight.
+__global__ __launch_bounds__(1024) void k_gn_bwd_merge(GnArgs A) {
+  __shared__ float red[32];
+  const int i = blockIdx.x / A.G, k = blockIdx.x - i * A.G;
   const float *const part = A.cpart + int64_t(i) * A.chunks1 * 2 * A.C + k * A.cg;
-  const int64_t count = int64_t(A.chunks1) * A.cg;
-  float s1 = 0.f, s2 = 0.f;
-  for (int64_t e = threadIdx.x; e < count; e += 64) {
-    const int64_t q = e / A.cg;
-    const int c = int(e - q * A.cg);
+  // S threads a channel, each every S-th chunk
+  const int S = max(1, int(blockDim.x) / A.cg);
+  float s[2] = {0.f, 0.f};
+  for (int e = threadIdx.x; e < A.cg * S; e += blockDim.x) {
+    const int r0 = e / A.cg, c = e - r0 * A.cg;
     const float ga = A.gamma[k * A.cg + c];
-    s2 += ga * part[q * 2 * A.C + c];
-    s1 += ga * part[q * 2 * A.C + A.C + c];
+    float t1 = 0.f, t2 = 0.f;
+    constexpr int U = 8;
+    for (int r = r0; r < A.chunks1; r += U * S) {
+      float v[2 * U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float *const q = part + int64_t(min(r + u * S, A.chunks1 - 1)) * 2 * A.C + c;
+        v[2 * u] = q[0];
+        v[2 * u + 1] = q[A.C];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        t2 += r + u * S < A.chunks1 ? v[2 * u] : 0.f;
+        t1 += r + u * S < A.chunks1 ? v[2 * u + 1] : 0.f;
+      }
+    }
+    s[0] += ga * t1;
+    s[1] += ga * t2;
   }
-  float s[2] = {s1, s2};
   add_from<2>(1, s);
-  if (threadIdx.x == 0) {
-    const float rstd = A.st[(A.n + i) * A.G + k];
-    A.gsum[2 * int64_t(blockIdx.x)] = rstd * s[0];
-    A.gsum[2 * int64_t(blockIdx.x) + 1] = rstd * s[1];
+  const int w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[w] = s[0];
+    red[16 + w] = s[1];
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    float t = 0.f;
+    for (int q = 0; q < nw; ++q) t += red[16 * threadIdx.x + q];
+    A.gsum[2 * int64_t(blockIdx.x) + threadIdx.x] = A.st[(A.n + i) * A.G + k] * t;
   }
 }
 
@@ -34,7 +58,10 @@ __global__ __launch_bounds__(1024) void k_gn_records(GnArgs A) {
 }  // namespace
 
 void merge_groups(hipStream_t s, const GnArgs &a) {
-  hipLaunchKernelGGL(k_gn_bwd_merge, dim3(uint32_t(a.n * a.G)), dim3(64), 0, s, a);
+  // as many wavefronts as hold about a chunk's row each
+  const int64_t work = int64_t(a.chunks1) * a.cg / 8;
+  const int threads = work >= 1024 ? 1024 : work >= 256 ? 256 : 64;
+  hipLaunchKernelGGL(k_gn_bwd_merge, dim3(uint32_t(a.n * a.G)), dim3(threads), 0, s, a);
 }
 
 void sum_records(hipStream_t s, const GnArgs &a) {
@@ -53,6 +80,7 @@ void gn_backward(hipStream_t s, const GnProblem &p, const GnPlan &plan, const vo
   GnArgs a = gn_args(p, plan.first, drop);
   a.rows = int(plan.rows);
   a.redbuf = plan.redbuf;
+  a.pack = plan.pack;
   a.x = x;
   a.g = g;
   a.out = d;

@@ -31,25 +31,30 @@ struct Column {
 };
 
 // Resident: one team per (sample, tile); a wavefront's loops over samples.
-template <typename XT, int V, int NV, int NJ, bool WAVE, bool POW2, bool SILU, bool DROP>
+template <typename XT, int V, int NV, int NJ, bool WAVE, int RED, bool SILU, bool DROP>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
   extern __shared__ float lds[];
   const Team<WAVE> tm(A);
   const int teams = WAVE ? blockDim.x / 64 : 1;
   const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles;
   const int c = tile * A.W + tm.tx * V;
-  const bool col = c < A.C && tm.ty < A.TY;
-  float *const red = lds + tm.index * (POW2 ? 2 : 1) * A.redbuf;
+  const bool column = tm.tx < A.cols && c < A.C;
+  float *const red = lds + tm.index * (RED == GN_RED_GROUPS ? 2 : 1) * A.redbuf;
   const DropKey key = drop_key(A.drop);
   const float m = float(A.hw * A.cg);  // exact: a team holds fewer than 2^24 values
-  for (int i = by * teams + tm.index; i < A.n; i = WAVE ? i + A.rows * teams : A.n) {
+  // a wavefront's rows are pixels, or samples of one
+  const bool packed = WAVE && A.pack > 1;
+  const int ty = packed ? 0 : tm.ty, step = A.rows * teams * (WAVE ? A.pack : 1);
+  for (int i0 = (by * teams + tm.index) * (WAVE ? A.pack : 1); i0 < A.n; i0 = WAVE ? i0 + step : A.n) {
+    const int i = packed ? i0 + tm.ty : i0;
+    const bool own = column && (!packed || i < A.n), col = own && ty < A.TY;
     const int64_t pix0 = int64_t(i) * A.hw;
-    const XT *const x = static_cast<const XT *>(A.x) + (pix0 + tm.ty) * A.ldx + c;
+    const XT *const x = static_cast<const XT *>(A.x) + (pix0 + ty) * A.ldx + c;
     const int64_t dx = int64_t(A.TY) * A.ldx;
     Vec<XT, V> xr[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (col && tm.ty + k * A.TY < A.hw) xr[k] = load_vec<XT, V>(x + k * dx);
+      if (col && ty + k * A.TY < A.hw) xr[k] = load_vec<XT, V>(x + k * dx);
     Column<XT, V, NJ> cp;
     float gamma[V];
 #pragma unroll
@@ -62,10 +67,10 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
     for (int j = 0; j < NJ; ++j) s[j] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (col && tm.ty + k * A.TY < A.hw)
+      if (col && ty + k * A.TY < A.hw)
 #pragma unroll
         for (int j = 0; j < V; ++j) s[NJ == 1 ? 0 : j] += float(xr[k].v[j]);
-    group_sums<1, NJ, V, WAVE, POW2>(A, tm, s, red);
+    group_sums<1, NJ, V, WAVE, RED>(A, tm, s, red);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       cp.mean[j] = s[j] / m;  // not times 1 / m: a constant group's mean is that constant
@@ -73,18 +78,18 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (col && tm.ty + k * A.TY < A.hw) {
+      if (col && ty + k * A.TY < A.hw) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float t = float(xr[k].v[j]) - cp.mean[NJ == 1 ? 0 : j];
           s[NJ == 1 ? 0 : j] += t * t;
         }
       }
-    group_sums<1, NJ, V, WAVE, POW2>(A, tm, s, red + (POW2 ? A.redbuf : 0));
+    group_sums<1, NJ, V, WAVE, RED>(A, tm, s, red + (RED == GN_RED_GROUPS ? A.redbuf : 0));
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) s[j] = 1.f / sqrtf(s[j] / m + A.eps);
+    for (int j = 0; j < NJ; ++j) s[j] = rsqrtf(s[j] * A.inv_m + A.eps);
     // the first thread of each group writes its statistics
-    if (tm.ty == 0 && c < A.C)
+    if (ty == 0 && own)
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         if (const int k = A.by_cg.of(c + j); k * A.cg == c + j) {
@@ -96,8 +101,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
       for (int j = 0; j < V; ++j) cp.a[j] = gamma[j] * s[NJ == 1 ? 0 : j];
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (tm.ty + k * A.TY < A.hw)
-          cp.template put<SILU, DROP>(A, key, xr[k], pix0 + tm.ty + k * A.TY, c);
+        if (ty + k * A.TY < A.hw)
+          cp.template put<SILU, DROP>(A, key, xr[k], pix0 + ty + k * A.TY, c);
     }
   }
 }
@@ -106,14 +111,15 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
 // thread sums differences from a pivot, its own first value: with the pivot
 // among the n values a thread sums, sum (x - pivot)^2 is at most n times their
 // squared differences from their mean, however far that is from zero.
-template <typename XT, int V, int NJ, bool POW2>
+template <typename XT, int V, int NJ, int RED>
 __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
   extern __shared__ float lds[];
   const Team<false> tm(A);
   const int by = A.by_tiles.of(blockIdx.x), tile = blockIdx.x - by * A.tiles;
   const int i = A.by_chunks.of(by), p0 = (by - i * A.chunks) * A.chunk, np = min(A.hw - p0, A.chunk);
   const int c = tile * A.W + tm.tx * V;
-  const int rows = c < A.C && tm.ty < A.TY && tm.ty < np ? (np - tm.ty + A.TY - 1) / A.TY : 0;
+  const bool own = tm.tx < A.cols && c < A.C;
+  const int rows = own && tm.ty < A.TY && tm.ty < np ? (np - tm.ty + A.TY - 1) / A.TY : 0;
   const XT *x = static_cast<const XT *>(A.x) + (int64_t(i) * A.hw + p0 + tm.ty) * A.ldx + c;
   const int64_t dx = int64_t(A.TY) * A.ldx;
   float pivot[NJ], s1[NJ], s2[NJ];
@@ -147,7 +153,7 @@ __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
     s2[j] = fmaxf(s2[j] - s1[j] * q, 0.f);
     s[j] = cnt * mean[j];
   }
-  group_sums<1, NJ, V, false, POW2>(A, tm, s, lds);
+  group_sums<1, NJ, V, false, RED>(A, tm, s, lds);
   float all[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
@@ -155,8 +161,8 @@ __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
     const float t = mean[j] - all[j];
     s[j] = s2[j] + cnt * t * t;
   }
-  group_sums<1, NJ, V, false, POW2>(A, tm, s, lds + (POW2 ? A.redbuf : 0));
-  if (tm.ty == 0 && c < A.C)
+  group_sums<1, NJ, V, false, RED>(A, tm, s, lds + (RED == GN_RED_GROUPS ? A.redbuf : 0));
+  if (tm.ty == 0 && own)
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
       if (const int k = A.by_cg.of(c + j); k * A.cg == c + j) {
@@ -202,7 +208,7 @@ __device__ __forceinline__ void merge_chunks(const GnArgs &A, int i, int k, int 
 #pragma unroll
   for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off);
   mean = float(mu);
-  rstd = 1.f / sqrtf(float(s / m) + A.eps);
+  rstd = rsqrtf(float(s / m) + A.eps);
 }
 
 // Many chunks: one wavefront per group of a sample.
@@ -324,11 +330,14 @@ void launch_resident(hipStream_t s, const GnPlan &g, const GnArgs &a) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, g.lds, s, a); };
   gn_choose(a, [&](auto silu, auto drop) {
     constexpr bool S = decltype(silu)::value, D = decltype(drop)::value;
-    // a wavefront's tile ends at 8 vectors a thread (gn_plan)
-    if constexpr (NV <= 8)
+    // a wavefront's tile ends at two vectors a thread (gn_plan)
+    if constexpr (NV <= 2)
       if (g.wave)
-        return g.pow2 ? go(k_gn_fwd<XT, V, NV, NJ, true, true, S, D>) : go(k_gn_fwd<XT, V, NV, NJ, true, false, S, D>);
-    g.pow2 ? go(k_gn_fwd<XT, V, NV, NJ, false, true, S, D>) : go(k_gn_fwd<XT, V, NV, NJ, false, false, S, D>);
+        return g.red == GN_RED_GROUPS ? go(k_gn_fwd<XT, V, NV, NJ, true, GN_RED_GROUPS, S, D>)
+                                      : go(k_gn_fwd<XT, V, NV, NJ, true, GN_RED_COLUMNS, S, D>);
+    g.red == GN_RED_GROUPS    ? go(k_gn_fwd<XT, V, NV, NJ, false, GN_RED_GROUPS, S, D>)
+    : g.red == GN_RED_COLUMNS ? go(k_gn_fwd<XT, V, NV, NJ, false, GN_RED_COLUMNS, S, D>)
+                              : go(k_gn_fwd<XT, V, NV, NJ, false, GN_RED_TREE, S, D>);
   });
 }
 
@@ -339,8 +348,8 @@ size_t apply_lds(const GnArgs &a, bool merge) {
 template <typename XT, int V, int NJ>
 void run_fwd(hipStream_t s, const GnProblem &p, const GnPlan &g, GnArgs a) {
   if (g.resident) {
-    if (V == 8 && g.NV <= 1) return launch_resident<XT, V, 1, NJ>(s, g, a);
-    if (V == 8 && g.NV <= 2) return launch_resident<XT, V, 2, NJ>(s, g, a);
+    if (g.NV <= 1) return launch_resident<XT, V, 1, NJ>(s, g, a);
+    if (g.NV <= 2) return launch_resident<XT, V, 2, NJ>(s, g, a);
     if (g.NV <= 4) return launch_resident<XT, V, 4, NJ>(s, g, a);
     if (g.NV <= 8) return launch_resident<XT, V, 8, NJ>(s, g, a);
     // fp32 vectors stop at 8 (gn_plan)
@@ -350,7 +359,9 @@ void run_fwd(hipStream_t s, const GnProblem &p, const GnPlan &g, GnArgs a) {
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(uint32_t(g.first.blocks)), dim3(g.first.threads), g.lds, s, a);
   };
-  g.pow2 ? go(k_gn_stats<XT, V, NJ, true>) : go(k_gn_stats<XT, V, NJ, false>);
+  g.red == GN_RED_GROUPS    ? go(k_gn_stats<XT, V, NJ, GN_RED_GROUPS>)
+  : g.red == GN_RED_COLUMNS ? go(k_gn_stats<XT, V, NJ, GN_RED_COLUMNS>)
+                            : go(k_gn_stats<XT, V, NJ, GN_RED_TREE>);
   GnArgs b = gn_args(p, g.second, a.drop);
   b.x = a.x;
   b.out = a.out;
@@ -386,6 +397,7 @@ void gn_forward(hipStream_t s, const GnProblem &p, const GnPlan &g, const void *
   GnArgs a = gn_args(p, g.first, drop);
   a.rows = int(g.rows);
   a.redbuf = g.redbuf;
+  a.pack = g.pack;
   a.x = x;
   a.out = y;
   a.ldo = p.ldy;

@@ -8,15 +8,23 @@
 namespace ckpt {
 namespace {
 
-bool is_pow2(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int vec_of(const GnProblem &p) { return p.C % 8 == 0 ? 8 : 1; }
 
-// Tiles of whole groups and whole vectors, about `want` channels each, at most
-// `cap` threads wide; V drops to 1 where a group is too wide for that.
-void group_tiles(const GnProblem &p, int64_t want, int cap8, GnCover &v) {
+int pow2_up(int v) {
+  int p = 1;
+  while (p < v) p *= 2;
+  return p;
+}
+
+// Tiles of whole groups and whole vectors, `want` channels or more each, at most
+// cap8 threads wide (1024 element by element); V drops to 1 where a group is too wide.
+// `lanes`: VC is rounded up to a power of two where it is at most 64, and the tile
+// taken (of up to four times the channels) whose columns fill it best, 7/8 or more
+// if any does.
+void group_tiles(const GnProblem &p, int64_t want, int cap8, bool lanes, GnCover &v) {
   v.V = vec_of(p);
   int64_t unit = std::lcm(int64_t(p.cg), int64_t(v.V));
   if (unit > 8 * 512) {
@@ -26,11 +34,20 @@ void group_tiles(const GnProblem &p, int64_t want, int cap8, GnCover &v) {
   const int64_t cap = v.V == 8 ? cap8 : 1024;
   if (unit / v.V > cap)
     fail(CKPT_E_UNSUPPORTED, "group norm: more than 1024 channels per group (4096 where 8 divides it)");
-  int64_t W = std::min(unit * ceil_div(want, unit), unit * std::max<int64_t>(1, cap * v.V / unit));
-  W = std::min<int64_t>(W, p.C);
-  v.W = int(W);
-  v.tiles = int(ceil_div(p.C, W));
-  v.VC = v.W / v.V;
+  const int64_t units = p.C / unit;  // whole: C is a multiple of cg and of V
+  int64_t m = std::min(std::min(ceil_div(want, unit), std::max<int64_t>(1, cap * v.V / unit)), units);
+  auto cols = [&](int64_t k) { return k * unit / v.V; };
+  if (lanes && cols(m) <= 64) {
+    int64_t best = m;
+    auto fill = [&](int64_t k) { return double(cols(k)) / pow2_up(int(cols(k))); };
+    for (int64_t k = m; k <= std::min(4 * m, units) && cols(k) <= 64 && fill(best) < 0.875; ++k)
+      if (fill(k) > fill(best)) best = k;
+    m = best;
+  }
+  v.W = int(m * unit);
+  v.tiles = int(ceil_div(p.C, v.W));
+  v.cols = v.W / v.V;
+  v.VC = lanes && v.cols <= 64 ? pow2_up(v.cols) : v.cols;
 }
 
 // chunks of a sample's pixels, about `blocks` workgroups in all, at least `least` rows
@@ -44,13 +61,13 @@ void cut(const GnProblem &p, int64_t blocks, int64_t least, GnCover &v) {
 
 void reductions(const GnProblem &p, bool backward, int NQ, GnPlan &g) {
   const GnCover &v = g.first;
-  g.pow2 = is_pow2(v.VC) && v.VC <= 64;
+  g.red = v.VC > 64 ? GN_RED_TREE : v.VC == v.cols ? GN_RED_GROUPS : GN_RED_COLUMNS;
   g.NJ = p.cg % v.V == 0 ? 1 : v.V;
   const int T = g.wave ? 64 : v.threads;
-  g.redbuf = NQ ? gn_reduce_floats(v, g.pow2, T, NQ, g.NJ, p.cg) : 0;
-  size_t f = size_t(g.pow2 ? 2 : 1) * g.teams * g.redbuf;
+  g.redbuf = NQ ? gn_reduce_floats(v, g.red, T, NQ, g.NJ, p.cg) : 0;
+  size_t f = size_t(g.red == GN_RED_GROUPS ? 2 : 1) * g.teams * g.redbuf;
   if (backward)  // the channels' sums
-    f = std::max(f, g.pow2 ? size_t(v.threads / 64) * 2 * v.W
+    f = std::max(f, g.red != GN_RED_TREE ? size_t(v.threads / 64) * 2 * v.V * v.VC
                            : size_t(g.teams) * (v.TY + (v.TY + 7) / 8) * v.VC * 2 * v.V);
   g.lds = 4 * f;
 }
@@ -61,13 +78,14 @@ GnCover gn_cover_elements(const GnProblem &p, int V, bool whole_groups) {
   GnCover v{};
   if (whole_groups) {
     // few enough channels for their parameters to stay in LDS
-    group_tiles(p, 512, 64, v);
+    group_tiles(p, 512, 64, false, v);
   } else {
     v.V = V;
     const int64_t vc = p.C / v.V;
     v.tiles = int(ceil_div(vc, 64));
     v.VC = int(ceil_div(vc, v.tiles));
     v.W = v.VC * v.V;
+    v.cols = v.VC;
   }
   v.threads = int(std::max<int64_t>(256, up(v.VC, 64)));
   v.TY = v.threads / v.VC;
@@ -92,11 +110,11 @@ GnCover gn_cover_rerun(const GnProblem &p) {
 GnPlan gn_plan(const GnProblem &p, bool backward) {
   GnPlan g{};
   GnCover &v = g.first;
-  g.teams = 1;
+  g.teams = g.pack = 1;
   // 128 bytes of a pixel at least, so that no two tiles share a cache line of
   // contiguous rows; more where a sample's pixels are too few for a wavefront
   const int64_t line = 128 / (p.xf ? 4 : 2);
-  group_tiles(p, std::max(line, ceil_div(64 * vec_of(p), p.hw)), backward ? 512 : 1024, v);
+  group_tiles(p, std::max(line, ceil_div(64 * vec_of(p), p.hw)), backward ? 512 : 1024, true, v);
   const int cap = backward && v.V == 8 ? 512 : 1024;
   const int64_t vecs = int64_t(v.VC) * p.hw, slabs = p.n * v.tiles;
   // vectors a thread keeps: 4 registers each for bf16, 8 for fp32 (and 8 more for
@@ -104,16 +122,23 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
   const int nv_max = v.V == 1 ? 16 : (backward || p.xf ? 8 : 16);
   v.chunks = 1;
   v.chunk = p.hw;
-  // a wavefront per sample and tile where there are enough of them to fill the
-  // device (4 a SIMD); else more threads share one
-  if (v.VC <= 64 && ceil_div(p.hw, 64 / v.VC) <= 8 && slabs >= 4096) {
+  // short samples, many of them: a wavefront per sample and tile, or for several
+  // samples of one pixel.  At four vectors a thread and more the workgroup form is
+  // faster (49 pixels x 64 channels, 2048 tiles: 16.8 us backward against 19.6).
+  if (v.VC <= 64 && ceil_div(p.hw, 64 / v.VC) <= 2 && slabs >= 1024) {
     g.resident = g.wave = true;
     g.teams = 4;
     v.threads = 256;
     v.TY = 64 / v.VC;
     g.NV = int(ceil_div(p.hw, v.TY));
-    // the workgroups loop over samples, so that few records of channel sums are left
-    g.rows = std::min<int64_t>(ceil_div(p.n, g.teams), std::max(1, 1024 / v.tiles));
+    reductions(p, backward, backward ? 2 : 1, g);
+    g.pack = p.hw == 1 && g.red == GN_RED_GROUPS && (g.NJ == 1 || p.cg == 2 || p.cg == 4) ? v.TY : 1;
+    const int64_t turns = ceil_div(p.n, int64_t(g.teams) * g.pack);  // of one workgroup
+    // the workgroups loop over samples: 1024 fill the device (2048 of 16384 rows of 1024
+    // channels: 31 us backward against 28), and a backward leaves at most half as many
+    // records of channel sums as it has turns
+    g.rows = std::min<int64_t>(turns, std::max(1, 1024 / v.tiles));
+    if (backward) g.rows = std::min(g.rows, std::max<int64_t>(std::min<int64_t>(turns, 64), ceil_div(turns, 2)));
   } else {
     v.threads = int(std::min<int64_t>(cap, up(v.VC * ceil_div(p.hw, 2), 64)));
     if (v.threads < v.VC) v.threads = int(up(v.VC, 64));
@@ -128,7 +153,7 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
   }
   if (g.resident) {
     v.blocks = g.rows * v.tiles;
-    reductions(p, backward, backward ? 2 : 1, g);
+    if (!g.wave) reductions(p, backward, backward ? 2 : 1, g);
     if (backward && g.rows > 1) g.ws_channels = align256(uint64_t(g.rows) * 2 * p.C * 4);
     return g;
   }
