@@ -674,6 +674,14 @@ def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=N
                   ldx, ldy, ldg, ldd, eps, 0)
 
 
+_Tensor = torch.Tensor
+
+
+def _ptr(x):
+    # a tensor first: these calls take a few microseconds in all
+    return x.data_ptr() if x.__class__ is _Tensor else _addr(x)
+
+
 def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
     v = C.c_uint64()
     _check(_lib.op_gn_workspace_bytes(desc, int(backward), C.byref(v)))
@@ -681,22 +689,22 @@ def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
 
 
 def op_gn_forward(desc, x, gamma, beta, y, st, workspace=None, workspace_bytes=0, drop=None, stream=None):
-    _check(_lib.op_gn_forward(desc, _addr(x), _addr(gamma), _addr(beta), drop, _addr(y), _addr(st),
-                              _addr(workspace), int(workspace_bytes), _s(stream)))
+    _check(_lib.op_gn_forward(desc, _ptr(x), _ptr(gamma), _ptr(beta), drop, _ptr(y), _ptr(st),
+                              _ptr(workspace), int(workspace_bytes), _s(stream)))
 
 
 def op_gn_apply(desc, x, st, gamma, beta, y, drop=None, stream=None):
-    _check(_lib.op_gn_apply(desc, _addr(x), _addr(st), _addr(gamma), _addr(beta), drop, _addr(y),
+    _check(_lib.op_gn_apply(desc, _ptr(x), _ptr(st), _ptr(gamma), _ptr(beta), drop, _ptr(y),
                             _s(stream)))
 
 
 def op_gn_backward(desc, g, x, st, gamma, beta, d, dgamma, dbeta, workspace=None, workspace_bytes=0, drop=None,
                    stream=None):
-    _check(_lib.op_gn_backward(desc, _addr(g), _addr(x), _addr(st), _addr(gamma), _addr(beta), drop,
-                               _addr(d), _addr(dgamma), _addr(dbeta), _addr(workspace), int(workspace_bytes),
+    _check(_lib.op_gn_backward(desc, _ptr(g), _ptr(x), _ptr(st), _ptr(gamma), _ptr(beta), drop,
+                               _ptr(d), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), int(workspace_bytes),
                                _s(stream)))
 
 
 def op_dropout(rows, cols, x, y, drop, res=None, xtype=TYPE_BF16, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
-    _check(_lib.op_dropout(rows, cols, xtype, _addr(x), ldx, _addr(res), ldr, xtype if ytype is None else ytype,
-                           _addr(y), ldy, drop, _s(stream)))
+    _check(_lib.op_dropout(rows, cols, xtype, _ptr(x), ldx, _ptr(res), ldr, xtype if ytype is None else ytype,
+                           _ptr(y), ldy, drop, _s(stream)))

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void k_gn_apply(GnArgs A) {
   const int64_t pix0 = int64_t(i) * A.hw + p0;
   const bool col = c < A.C && ty < A.TY;
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
-  constexpr int U = 4;
+  constexpr int U = 2;  // vectors worked on, and as many in flight
   Vec<XT, V> xr[U];
 #pragma unroll
   for (int k = 0; k < U; ++k)

@@ -91,6 +91,8 @@ GnCover gn_cover_elements(const GnProblem &p, int V, bool whole_groups) {
   v.TY = v.threads / v.VC;
   v.TY = int(std::min<int64_t>(v.TY, p.hw));
   v.threads = int(up(int64_t(v.TY) * v.VC, 64));
+  // four workgroups a CU, one turn: each forms its channels' parameters once (the stem's
+  // forward: 33 us, 35 at 2048, 47 at 4096)
   cut(p, 1024, 4, v);
   return v;
 }
@@ -140,12 +142,17 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
     g.rows = std::min<int64_t>(turns, std::max(1, 1024 / v.tiles));
     if (backward) g.rows = std::min(g.rows, std::max<int64_t>(std::min<int64_t>(turns, 64), ceil_div(turns, 2)));
   } else {
+    // two vectors a thread while the workgroup may grow (one sample of 49 pixels x 512
+    // channels, forward: 3.9 us; at four vectors 4.6, at eight 5.8)
     v.threads = int(std::min<int64_t>(cap, up(v.VC * ceil_div(p.hw, 2), 64)));
     if (v.threads < v.VC) v.threads = int(up(v.VC, 64));
     v.TY = v.threads / v.VC;
     const int64_t nv = ceil_div(p.hw, v.TY);
     // few slabs only while one is read in a few microseconds by its one compute unit
-    if (nv <= nv_max && (slabs >= 128 || vecs <= 4096)) {
+    // (bf16 forward, microseconds resident and split: 4 slabs of 3200 vectors 7.4 and
+    // 8.7, of 6272 vectors 10.7 and 8.8; 32 of them 11.1 and 9.6, 64 11.9 and 12.4; 256
+    // 20.0 and 24.8)
+    if (nv <= nv_max && (slabs >= 64 || vecs <= 4096)) {
       g.resident = true;
       g.NV = int(nv);
       g.rows = p.n;
@@ -159,13 +166,20 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
   }
   v.threads = int(std::max<int64_t>(256, up(v.VC, 64)));
   v.TY = v.threads / v.VC;
+  // two workgroups a CU: fewer chunks to add up outweigh the latency that four would
+  // hide (stage-1 backward with dropout: 61 us, 64 at 1024)
   cut(p, 512, 4, v);
   reductions(p, backward, backward ? 0 : 1, g);
   if (backward) {
+    // adding up the chunks costs every workgroup of the second pass more the more there
+    // are (196 of them: 27.7 us, 17.5 with a launch for it; 49: 13.7 and 12.5), and
+    // groups wider than a tile have to be formed outside
     g.merge = v.chunks > 32 || p.cg > 64;
     g.ws_channels = align256(uint64_t(p.n) * v.chunks * 2 * p.C * 4);
     if (g.merge) g.ws_sums = align256(uint64_t(p.n) * p.G * 8);
   } else {
+    // (98 chunks: 13.1 us in the second pass, 10.2 with a launch; 64 or fewer are read at
+    // once)
     g.merge = v.chunks > 64;
     g.ws_groups = align256(uint64_t(p.n) * v.chunks * p.G * 8);
   }
