@@ -662,6 +662,8 @@ def type_of(t) -> int:
 def dropout(rng, p: float, site: int = 0) -> Dropout:
     """Dropout with the {seed, step} pair at `rng` (device int64 or uint64 [2],
     kept alive by the result)."""
+    if not 0 <= site < 1 << 32:
+        raise CkptError(E_INVALID, "dropout: site must lie in [0, 2^32)")
     d = Dropout(_addr(rng), site, 0, p)
     d._keep = rng
     return d
@@ -670,6 +672,8 @@ def dropout(rng, p: float, site: int = 0) -> Dropout:
 def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=None, ldx=0, ldy=0, ldg=0, ldd=0,
             eps=1e-5) -> GnDesc:
     """gtype and dtype default to xtype, strides to c."""
+    if max(n, hw, c, groups, ldx, ldy, ldg, ldd) >= 1 << 62 or max(c, groups) >= 1 << 31:
+        raise CkptError(E_UNSUPPORTED, "gn_desc: a size does not fit its field")
     return GnDesc(n, hw, c, groups, act, xtype, xtype if gtype is None else gtype, xtype if dtype is None else dtype,
                   ldx, ldy, ldg, ldd, eps, 0)
 

@@ -159,6 +159,26 @@ def test_calls_refused(call, code):
     assert e.value.code == code and K._lib.ckpt_last_error()
 
 
+@pytest.mark.parametrize("make,code", [
+    (lambda: K.dropout(FAKE, 0.1, 1 << 32), K.E_INVALID), (lambda: K.dropout(FAKE, 0.1, -1), K.E_INVALID),
+    (lambda: _d(c=(1 << 32) + 16), K.E_UNSUPPORTED), (lambda: _d(groups=1 << 31), K.E_UNSUPPORTED),
+    (lambda: _d(n=1 << 64), K.E_UNSUPPORTED),
+])
+def test_sizes_that_do_not_fit_their_fields(make, code):
+    with pytest.raises(K.CkptError) as e:
+        make()
+    assert e.value.code == code
+
+
+def test_too_many_workgroups_refused():
+    for call in (lambda d: K.op_gn_forward(d, FAKE, FAKE, FAKE, FAKE, FAKE),
+                 lambda d: K.op_gn_apply(d, FAKE, FAKE, FAKE, FAKE, FAKE),
+                 lambda d: K.op_gn_backward(d, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 60)):
+        with pytest.raises(K.CkptError) as e:
+            call(_d(n=1 << 22, hw=200, c=8, groups=1))
+        assert e.value.code == K.E_UNSUPPORTED
+
+
 def test_type_of_refuses_other_types():
     import torch
     with pytest.raises(K.CkptError) as e:

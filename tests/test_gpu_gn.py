@@ -5,10 +5,10 @@ Bars, per element: half a step of the output's type at the exact value (bf16
 2^-8 of it, fp32 2^-24) for the one rounding at the end, plus
 L 2^-24 times the sum of the magnitudes that enter the element, for the fp32
 arithmetic.  L bounds the operations an input passes: a sum runs over at most
-128 values in a thread (16 vectors of 8), then trees of eight of at most 1024
-threads, 16 wavefronts or 64 columns, and 64 records in turn, below 256 in all;
-the few operations before and after it are covered by the distance of 256 to
-these 240.  ReLU's decisions are the documented fp32 ones (oracle.affine_f32).
+128 values in a thread (16 vectors of 8; the chunks of the sizes here are no
+longer), then trees of eight of at most 1024 threads, 16 wavefronts or 64
+columns, and 64 records in turn, below 256 in all; the few operations before and
+after it are covered by the distance of 256 to these 240.  ReLU's decisions are the documented fp32 ones (oracle.affine_f32).
 """
 import numpy as np
 import pytest
@@ -211,6 +211,15 @@ SHAPES = {
     "scalar_wide": (1, 130, 515, 1),
     "one_channel": (3, 50, 1, 1),
     "last_tile_short": (2, 60, 200, 25),
+    "rows_packed": (4100, 1, 64, 4),       # eight samples of one pixel a wavefront
+    "rows_packed_fours": (2101, 1, 32, 8),
+    "rows_packed_pairs": (3003, 1, 16, 8),
+    "fours": (3, 300, 64, 16),             # groups of four channels, two in a vector
+    "padded_columns": (2, 100, 320, 32),   # ten channels a group: 15 of 16 columns in use
+    "padded_one_group": (3, 70, 40, 1),
+    "split_many_chunks": (1, 40000, 64, 8),
+    "split_wide_groups": (1, 9000, 256, 2),
+    "split_one_wide": (1, 3000, 1024, 1),
 }
 
 
