@@ -211,7 +211,9 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
   const bool col = tm.tx < A.cols && c < A.C && tm.ty < A.TY;
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
   const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
-  constexpr int U = 1;
+  // vectors in flight besides those worked on: more cost registers that hide the
+  // arithmetic better (stage 1 with dropout: 59 us, 62 with two)
+  constexpr int U = V == 1 ? 4 : 1;
   Vec<XT, V> xr[U];
   Vec<GT_, V> gr[U];
 #pragma unroll
@@ -229,8 +231,38 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
   if (col) {
     Column<XT, V, V> cp;
     take_params(A, tm.tx, lds, cp);
+    auto add = [&](auto silu, auto drop, const Vec<XT, V> &xv, const Vec<GT_, V> &gv, int p) {
+      float du[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) du[j] = float(gv.v[j]);
+      cp.template du<silu.value, drop.value>(A, key, xv, uint64_t(pix0 + p), c, du);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        ch[j] += du[j] * (float(xv.v[j]) - cp.mean[j]);
+        ch[V + j] += du[j];
+      }
+    };
     gn_choose(A, [&](auto silu, auto drop) {
-      for (int r = tm.ty; r < np; r += U * A.TY) {
+      int r = tm.ty;
+      // element by element, while every thread has all its pixels (k_gn_apply; vectors
+      // lose by it, their time is arithmetic: stage 1 with dropout 59 -> 64 us)
+      for (int q = 2 * U * A.TY; V == 1 && q <= np; q += U * A.TY, r += U * A.TY) {
+        Vec<XT, V> nx[U];
+        Vec<GT_, V> ng[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          nx[k] = load_vec<XT, V>(x + int64_t(r + (U + k) * A.TY) * A.ldx);
+          ng[k] = load_vec<GT_, V>(g + int64_t(r + (U + k) * A.TY) * A.ldg);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) add(silu, drop, xr[k], gr[k], r + k * A.TY);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          xr[k] = nx[k];
+          gr[k] = ng[k];
+        }
+      }
+      for (; r < np; r += U * A.TY) {
         Vec<XT, V> nx[U];
         Vec<GT_, V> ng[U];
 #pragma unroll
@@ -241,17 +273,7 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
           }
 #pragma unroll
         for (int k = 0; k < U; ++k)
-          if (r + k * A.TY < np) {
-            float du[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) du[j] = float(gr[k].v[j]);
-            cp.template du<silu.value, drop.value>(A, key, xr[k], uint64_t(pix0 + r + k * A.TY), c, du);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              ch[j] += du[j] * (float(xr[k].v[j]) - cp.mean[j]);
-              ch[V + j] += du[j];
-            }
-          }
+          if (r + k * A.TY < np) add(silu, drop, xr[k], gr[k], r + k * A.TY);
 #pragma unroll
         for (int k = 0; k < U; ++k) {
           xr[k] = nx[k];
@@ -305,7 +327,7 @@ __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, 
   const bool col = c < A.C && ty < A.TY;
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
   const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
-  constexpr int U = 1;
+  constexpr int U = V == 1 ? 4 : 1;
   Vec<XT, V> xr[U];
   Vec<GT_, V> gr[U];
 #pragma unroll
@@ -373,8 +395,32 @@ __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, 
     k1[j] = kk[tx * V + j];
     k2[j] = kk[A.W + tx * V + j];
   }
+  auto form = [&](auto silu, auto drop, const Vec<XT, V> &xv, const Vec<GT_, V> &gv, int p) {
+    float du[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) du[j] = float(gv.v[j]);
+    cp.template du<silu.value, drop.value>(A, key, xv, uint64_t(pix0 + p), c, du);
+    cp.template put<DT>(A, xv, k1, k2, pix0 + p, c, du);
+  };
   gn_choose(A, [&](auto silu, auto drop) {
-    for (int r = ty; r < np; r += U * A.TY) {
+    int r = ty;
+    for (int q = 2 * U * A.TY; V == 1 && q <= np; q += U * A.TY, r += U * A.TY) {  // as in the first pass
+      Vec<XT, V> nx[U];
+      Vec<GT_, V> ng[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        nx[k] = load_vec<XT, V>(x + int64_t(r + (U + k) * A.TY) * A.ldx);
+        ng[k] = load_vec<GT_, V>(g + int64_t(r + (U + k) * A.TY) * A.ldg);
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) form(silu, drop, xr[k], gr[k], r + k * A.TY);
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        xr[k] = nx[k];
+        gr[k] = ng[k];
+      }
+    }
+    for (; r < np; r += U * A.TY) {
       Vec<XT, V> nx[U];
       Vec<GT_, V> ng[U];
 #pragma unroll
@@ -385,13 +431,7 @@ __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, 
         }
 #pragma unroll
       for (int k = 0; k < U; ++k)
-        if (r + k * A.TY < np) {
-          float du[V];
-#pragma unroll
-          for (int j = 0; j < V; ++j) du[j] = float(gr[k].v[j]);
-          cp.template du<silu.value, drop.value>(A, key, xr[k], uint64_t(pix0 + r + k * A.TY), c, du);
-          cp.template put<DT>(A, xr[k], k1, k2, pix0 + r + k * A.TY, c, du);
-        }
+        if (r + k * A.TY < np) form(silu, drop, xr[k], gr[k], r + k * A.TY);
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         xr[k] = nx[k];
