@@ -85,10 +85,19 @@ __device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE>
   }
 }
 
+// Wavefronts a SIMD that a resident kernel's registers leave room for: 4 (128
+// registers), 2 where its vectors, or the sums of eight channels that a wavefront
+// keeps from sample to sample, take more (2048 samples of 16 pixels x 64 channels in
+// groups of four: 17.1 us held to 128 registers, 11.9 not).
+template <int V, int NV, int NJ, bool WAVE>
+constexpr int gnb_waves() {
+  return V == 8 && (NV >= 4 || (WAVE && NJ > 1)) ? 2 : 4;
+}
+
 // Resident: one team per (sample, tile); a wavefront's loops over samples.
 template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, int RED, bool SILU,
           bool DROP>
-__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, V == 8 && NV >= 4 ? 2 : 4) void k_gn_bwd(GnArgs A) {
+__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, gnb_waves<V, NV, NJ, WAVE>()) void k_gn_bwd(GnArgs A) {
   extern __shared__ float lds[];
   const Team<WAVE> tm(A);
   const int teams = WAVE ? blockDim.x / 64 : 1;
