@@ -95,7 +95,7 @@ struct GnArgs {
   float *st;     // mean [n G] | rstd [n G]
   float *gpart;  // forward, split: [n][chunks][G] (mean, squared differences) of the first pass's chunks
   float *cpart;  // backward: [rows][2][C] of the channels (sum du xhat | sum du)
-  float *gsum;   // backward, split and merged: [n][G] (S1, S2)
+  float *gsum;   // backward, split and merged: [n][G] (sum a du, sum a du xhat)
   float *dgamma, *dbeta;
   int n, hw, rows;
   int chunks, chunk;    // this pass's

@@ -97,7 +97,7 @@ constexpr int gnb_waves() {
 // Resident: one team per (sample, tile); a wavefront's loops over samples.
 template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, int RED, bool SILU,
           bool DROP>
-__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, gnb_waves<V, NV, NJ, WAVE>()) void k_gn_bwd(GnArgs A) {
+__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, (gnb_waves<V, NV, NJ, WAVE>())) void k_gn_bwd(GnArgs A) {
   extern __shared__ float lds[];
   const Team<WAVE> tm(A);
   const int teams = WAVE ? blockDim.x / 64 : 1;
