@@ -108,9 +108,16 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
 }
 
 // Split, first pass: a chunk's mean and squared differences per group.  Each
-// thread sums differences from a pivot, its own first value: with the pivot
-// among the n values a thread sums, sum (x - pivot)^2 is at most n times their
-// squared differences from their mean, however far that is from zero.
+// thread sums differences from a pivot, and their squares, block by block of its
+// rows; a block of n2 values joins the n1 before it, whose mean is its pivot, by
+//   mean += s1 / (n1 + n2), M2 += s2 - s1^2 / (n1 + n2)
+// which is Chan's formula (gn_apply) for such a pivot.  A block is as long as all
+// before it, and 256 values at most: s1^2 / (n1 + n2) <= s2 n2 / (n1 + n2) is then at
+// most half of s2, whatever the values.  (The first block's pivot is the mean of eight
+// of its 32 values, or one of its 16: at most fifteen sixteenths.)  A single pivot for
+// a whole chunk would cancel by the number of its values where the first of them is
+// far from the others (1 / std off by 3e-4 at 784 values a thread, 1e-2 at 3136; 3e-7
+// this way, in the same time).
 template <typename XT, int V, int NJ, int RED>
 __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
   extern __shared__ float lds[];
@@ -122,15 +129,16 @@ __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
   const int rows = own && tm.ty < A.TY && tm.ty < np ? (np - tm.ty + A.TY - 1) / A.TY : 0;
   const XT *x = static_cast<const XT *>(A.x) + (int64_t(i) * A.hw + p0 + tm.ty) * A.ldx + c;
   const int64_t dx = int64_t(A.TY) * A.ldx;
-  float pivot[NJ], s1[NJ], s2[NJ];
+  // mean: the pivot, `low` what its roundings left (one at every block)
+  float mean[NJ], low[NJ], m2[NJ], s1[NJ], s2[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) pivot[j] = s1[j] = s2[j] = 0.f;
+  for (int j = 0; j < NJ; ++j) mean[j] = low[j] = m2[j] = 0.f;
   // (eight single elements in flight: a load instruction moves an eighth of a vector's)
   constexpr int U = V == 1 ? 8 : 4;
   auto add = [&](const Vec<XT, V> &v) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float t = float(v.v[j]) - pivot[NJ == 1 ? 0 : j];
+      const float t = float(v.v[j]) - mean[NJ == 1 ? 0 : j];
       s1[NJ == 1 ? 0 : j] += t;
       s2[NJ == 1 ? 0 : j] += t * t;
     }
@@ -138,33 +146,45 @@ __global__ __launch_bounds__(1024) void k_gn_stats(GnArgs A) {
   if (rows > 0) {
     const Vec<XT, V> v = load_vec<XT, V>(x);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) pivot[j] = float(v.v[j]);
+    for (int j = 0; j < V; ++j) mean[NJ == 1 ? 0 : j] += NJ == 1 ? float(v.v[j]) * (1.f / V) : float(v.v[j]);
   }
-  int r = 0;
-  for (; r + U <= rows; r += U, x += U * dx) {
-    Vec<XT, V> xr[U];
+  constexpr int E = NJ == 1 ? V : 1;  // values a row adds to a sum
+  for (int r = 0; r < rows;) {
+    const int end = min(rows, r + (r ? min(r, 256 / E) : E == 8 ? 4 : 16));
 #pragma unroll
-    for (int k = 0; k < U; ++k) xr[k] = load_vec<XT, V>(x + k * dx);
+    for (int j = 0; j < NJ; ++j) s1[j] = s2[j] = 0.f;
+    for (; r + U <= end; r += U, x += U * dx) {
+      Vec<XT, V> xr[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k) add(xr[k]);
+      for (int k = 0; k < U; ++k) xr[k] = load_vec<XT, V>(x + k * dx);
+      // all of them before the first wait: to save registers the compiler would
+      // take them one by one (128 x 3136 pixels x 72 channels in 24 groups: 50 us, 39)
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < U; ++k) add(xr[k]);
+    }
+    for (; r < end; ++r, x += dx) add(load_vec<XT, V>(x));
+    const float inv = 1.f / float(r * E);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float q = s1[j] * inv, step = q + low[j], sum = mean[j] + step, part = sum - mean[j];
+      low[j] = (mean[j] - (sum - part)) + (step - part);
+      mean[j] = sum;
+      // squares past fp32's range stay so (finite ones are at least s1 q)
+      m2[j] += s2[j] <= 3.4028234e38f ? fmaxf(s2[j] - s1[j] * q, 0.f) : s2[j];
+    }
   }
-  for (; r < rows; ++r, x += dx) add(load_vec<XT, V>(x));
-  const float cnt = float(rows * (NJ == 1 ? V : 1)), m = float(int64_t(np) * A.cg);
-  float mean[NJ], s[NJ];
+  const float cnt = float(rows * E), m = float(int64_t(np) * A.cg);
+  float s[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const float q = rows ? s1[j] / cnt : 0.f;
-    mean[j] = pivot[j] + q;
-    s2[j] = fmaxf(s2[j] - s1[j] * q, 0.f);
-    s[j] = cnt * mean[j];
-  }
+  for (int j = 0; j < NJ; ++j) s[j] = cnt * mean[j];
   group_sums<1, NJ, V, false, RED>(A, tm, s, lds);
   float all[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     all[j] = s[j] / m;
     const float t = mean[j] - all[j];
-    s[j] = s2[j] + cnt * t * t;
+    s[j] = m2[j] + cnt * t * t;
   }
   group_sums<1, NJ, V, false, RED>(A, tm, s, lds + (RED == GN_RED_GROUPS ? A.redbuf : 0));
   if (tm.ty == 0 && own)
