@@ -649,6 +649,7 @@ def op_maxpool(backward, n, h, w, c, ho, wo, r, out, g=None, y=None, arg=None, s
 
 # ------------------------------------------------- group norm and dropout --
 _TYPE_CODES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+_TYPE_NAMES = {code: t for t, code in _TYPE_CODES.items()}
 
 
 def type_of(t) -> int:
@@ -664,6 +665,10 @@ def dropout(rng, p: float, site: int = 0) -> Dropout:
     kept alive by the result)."""
     if not 0 <= site < 1 << 32:
         raise CkptError(E_INVALID, "dropout: site must lie in [0, 2^32)")
+    if isinstance(rng, torch.Tensor) and (rng.dtype.is_floating_point or not rng.is_contiguous() or
+                                          rng.numel() * rng.element_size() < 16):
+        raise CkptError(E_INVALID, f"dropout: seed and step are two 64-bit integers side by side, not {rng.dtype} of "
+                                   f"shape {tuple(rng.shape)}, strides {rng.stride()}")
     d = Dropout(_addr(rng), site, 0, p)
     d._keep = rng
     return d
@@ -681,9 +686,20 @@ def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=N
 _Tensor = torch.Tensor
 
 
-def _ptr(x):
-    # a tensor first: these calls take a few microseconds in all
-    return x.data_ptr() if x.__class__ is _Tensor else _addr(x)
+def _typed(x, code, name):
+    """The address of x, in tensors of the type `code` (None: any).  Addresses and
+    memory without a floating-point type are taken as they are."""
+    if isinstance(x, _Tensor):
+        t = x.dtype
+        if code is not None and t.is_floating_point and _TYPE_CODES.get(t) != code:
+            raise CkptError(E_INVALID, f"{name}: a tensor of {t}, described as {_TYPE_NAMES.get(code, code)}")
+        return x.data_ptr()
+    return _addr(x)
+
+
+def _type_or(x, code) -> int:
+    """The type code of a floating-point tensor, else `code`."""
+    return type_of(x) if isinstance(x, _Tensor) and x.dtype.is_floating_point else code
 
 
 def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
@@ -693,22 +709,32 @@ def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
 
 
 def op_gn_forward(desc, x, gamma, beta, y, st, workspace=None, workspace_bytes=0, drop=None, stream=None):
-    _check(_lib.op_gn_forward(desc, _ptr(x), _ptr(gamma), _ptr(beta), drop, _ptr(y), _ptr(st),
-                              _ptr(workspace), int(workspace_bytes), _s(stream)))
+    xt = getattr(desc, "xtype", None)
+    _check(_lib.op_gn_forward(desc, _typed(x, xt, "x"), _typed(gamma, TYPE_F32, "gamma"), _typed(beta, TYPE_F32, "beta"),
+                              drop, _typed(y, xt, "y"), _typed(st, TYPE_F32, "st"), _addr(workspace),
+                              int(workspace_bytes), _s(stream)))
 
 
 def op_gn_apply(desc, x, st, gamma, beta, y, drop=None, stream=None):
-    _check(_lib.op_gn_apply(desc, _ptr(x), _ptr(st), _ptr(gamma), _ptr(beta), drop, _ptr(y),
-                            _s(stream)))
+    xt = getattr(desc, "xtype", None)
+    _check(_lib.op_gn_apply(desc, _typed(x, xt, "x"), _typed(st, TYPE_F32, "st"), _typed(gamma, TYPE_F32, "gamma"),
+                            _typed(beta, TYPE_F32, "beta"), drop, _typed(y, xt, "y"), _s(stream)))
 
 
 def op_gn_backward(desc, g, x, st, gamma, beta, d, dgamma, dbeta, workspace=None, workspace_bytes=0, drop=None,
                    stream=None):
-    _check(_lib.op_gn_backward(desc, _ptr(g), _ptr(x), _ptr(st), _ptr(gamma), _ptr(beta), drop,
-                               _ptr(d), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), int(workspace_bytes),
-                               _s(stream)))
+    _check(_lib.op_gn_backward(desc, _typed(g, getattr(desc, "gtype", None), "g"),
+                               _typed(x, getattr(desc, "xtype", None), "x"), _typed(st, TYPE_F32, "st"),
+                               _typed(gamma, TYPE_F32, "gamma"), _typed(beta, TYPE_F32, "beta"), drop,
+                               _typed(d, getattr(desc, "dtype", None), "d"), _typed(dgamma, TYPE_F32, "dgamma"),
+                               _typed(dbeta, TYPE_F32, "dbeta"), _addr(workspace), int(workspace_bytes), _s(stream)))
 
 
-def op_dropout(rows, cols, x, y, drop, res=None, xtype=TYPE_BF16, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
-    _check(_lib.op_dropout(rows, cols, xtype, _ptr(x), ldx, _ptr(res), ldr, xtype if ytype is None else ytype,
-                           _ptr(y), ldy, drop, _s(stream)))
+def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
+    """xtype and ytype default to the tensors' types; for addresses to bf16 and to xtype."""
+    if xtype is None:
+        xtype = _type_or(x, TYPE_BF16)
+    if ytype is None:
+        ytype = _type_or(y, xtype)
+    _check(_lib.op_dropout(rows, cols, xtype, _typed(x, xtype, "x"), ldx, _typed(res, ytype, "res"), ldr, ytype,
+                           _typed(y, ytype, "y"), ldy, drop, _s(stream)))
