@@ -674,32 +674,45 @@ def dropout(rng, p: float, site: int = 0) -> Dropout:
     return d
 
 
+def _fit(what, bits, *values, large=E_UNSUPPORTED):
+    # ctypes keeps a value's low bits alone
+    if max(values) >= 1 << bits:
+        raise CkptError(large, f"{what}: a value does not fit its field")
+    if min(values) < -(1 << bits):
+        raise CkptError(E_INVALID, f"{what}: a value does not fit its field")
+
+
 def gn_desc(n, hw, c, groups, act=ACT_NONE, xtype=TYPE_BF16, gtype=None, dtype=None, ldx=0, ldy=0, ldg=0, ldd=0,
             eps=1e-5) -> GnDesc:
     """gtype and dtype default to xtype, strides to c."""
-    if max(n, hw, c, groups, ldx, ldy, ldg, ldd) >= 1 << 62 or max(c, groups) >= 1 << 31:
-        raise CkptError(E_UNSUPPORTED, "gn_desc: a size does not fit its field")
-    return GnDesc(n, hw, c, groups, act, xtype, xtype if gtype is None else gtype, xtype if dtype is None else dtype,
-                  ldx, ldy, ldg, ldd, eps, 0)
+    types = xtype, xtype if gtype is None else gtype, xtype if dtype is None else dtype
+    _fit("gn_desc", 62, n, hw, ldx, ldy, ldg, ldd)
+    _fit("gn_desc", 31, c, groups)
+    _fit("gn_desc: act and types", 31, act, *types, large=E_INVALID)
+    return GnDesc(n, hw, c, groups, act, *types, ldx, ldy, ldg, ldd, eps, 0)
 
 
-_Tensor = torch.Tensor
+_F32 = torch.float32
 
 
-def _typed(x, code, name):
-    """The address of x, in tensors of the type `code` (None: any).  Addresses and
-    memory without a floating-point type are taken as they are."""
-    if isinstance(x, _Tensor):
-        t = x.dtype
-        if code is not None and t.is_floating_point and _TYPE_CODES.get(t) != code:
-            raise CkptError(E_INVALID, f"{name}: a tensor of {t}, described as {_TYPE_NAMES.get(code, code)}")
-        return x.data_ptr()
-    return _addr(x)
+def _typed(*args):
+    """The addresses of (x, type, name)s; a floating-point tensor is refused if it is not
+    of its type (None: any), addresses and other memory are taken as they are."""
+    for x, want, name in args:
+        if isinstance(x, torch.Tensor) and want is not None and x.dtype.is_floating_point and x.dtype is not want:
+            raise CkptError(E_INVALID, f"{name}: a tensor of {x.dtype}, described as {want}")
+    return [_addr(x) for x, _, _ in args]
+
+
+def _described(desc):
+    """The types of g, x and d (None: not one, or not given as a GnDesc)."""
+    name = _TYPE_NAMES.get
+    return [name(getattr(desc, k, None)) for k in ("gtype", "xtype", "dtype")]
 
 
 def _type_or(x, code) -> int:
     """The type code of a floating-point tensor, else `code`."""
-    return type_of(x) if isinstance(x, _Tensor) and x.dtype.is_floating_point else code
+    return type_of(x) if isinstance(x, torch.Tensor) and x.dtype.is_floating_point else code
 
 
 def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
@@ -708,26 +721,70 @@ def op_gn_workspace_bytes(desc: GnDesc, backward: bool) -> int:
     return v.value
 
 
+def _nbytes(v) -> int:
+    if not 0 <= v < 1 << 64:
+        raise CkptError(E_INVALID, f"workspace_bytes: {v}")
+    return int(v)
+
+
+# The calls below take a few microseconds in all: where everything is a tensor of its
+# type, that is seen at once (an unknown type code is the library's to refuse), and the
+# checks that name what is wrong are made only where it is not.
+_DTYPES = torch.float32, torch.bfloat16  # by type code
+
+
 def op_gn_forward(desc, x, gamma, beta, y, st, workspace=None, workspace_bytes=0, drop=None, stream=None):
-    xt = getattr(desc, "xtype", None)
-    _check(_lib.op_gn_forward(desc, _typed(x, xt, "x"), _typed(gamma, TYPE_F32, "gamma"), _typed(beta, TYPE_F32, "beta"),
-                              drop, _typed(y, xt, "y"), _typed(st, TYPE_F32, "st"), _addr(workspace),
-                              int(workspace_bytes), _s(stream)))
+    try:
+        xt = _DTYPES[desc.xtype]
+        plain = x.dtype is xt and y.dtype is xt and gamma.dtype is _F32 and beta.dtype is _F32 and st.dtype is _F32
+    except (AttributeError, IndexError):
+        plain = False
+    if plain:
+        px, pg, pb, py, ps = x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr(), st.data_ptr()
+    else:
+        _, xt, _ = _described(desc)
+        px, pg, pb, py, ps = _typed((x, xt, "x"), (gamma, _F32, "gamma"), (beta, _F32, "beta"), (y, xt, "y"),
+                                    (st, _F32, "st"))
+    if workspace_bytes:
+        workspace_bytes = _nbytes(workspace_bytes)
+    _check(_lib.op_gn_forward(desc, px, pg, pb, drop, py, ps, _addr(workspace), workspace_bytes, _s(stream)))
 
 
 def op_gn_apply(desc, x, st, gamma, beta, y, drop=None, stream=None):
-    xt = getattr(desc, "xtype", None)
-    _check(_lib.op_gn_apply(desc, _typed(x, xt, "x"), _typed(st, TYPE_F32, "st"), _typed(gamma, TYPE_F32, "gamma"),
-                            _typed(beta, TYPE_F32, "beta"), drop, _typed(y, xt, "y"), _s(stream)))
+    try:
+        xt = _DTYPES[desc.xtype]
+        plain = x.dtype is xt and y.dtype is xt and gamma.dtype is _F32 and beta.dtype is _F32 and st.dtype is _F32
+    except (AttributeError, IndexError):
+        plain = False
+    if plain:
+        px, ps, pg, pb, py = x.data_ptr(), st.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr()
+    else:
+        _, xt, _ = _described(desc)
+        px, ps, pg, pb, py = _typed((x, xt, "x"), (st, _F32, "st"), (gamma, _F32, "gamma"), (beta, _F32, "beta"),
+                                    (y, xt, "y"))
+    _check(_lib.op_gn_apply(desc, px, ps, pg, pb, drop, py, _s(stream)))
 
 
 def op_gn_backward(desc, g, x, st, gamma, beta, d, dgamma, dbeta, workspace=None, workspace_bytes=0, drop=None,
                    stream=None):
-    _check(_lib.op_gn_backward(desc, _typed(g, getattr(desc, "gtype", None), "g"),
-                               _typed(x, getattr(desc, "xtype", None), "x"), _typed(st, TYPE_F32, "st"),
-                               _typed(gamma, TYPE_F32, "gamma"), _typed(beta, TYPE_F32, "beta"), drop,
-                               _typed(d, getattr(desc, "dtype", None), "d"), _typed(dgamma, TYPE_F32, "dgamma"),
-                               _typed(dbeta, TYPE_F32, "dbeta"), _addr(workspace), int(workspace_bytes), _s(stream)))
+    try:
+        plain = (g.dtype is _DTYPES[desc.gtype] and x.dtype is _DTYPES[desc.xtype] and d.dtype is _DTYPES[desc.dtype] and
+                 st.dtype is _F32 and gamma.dtype is _F32 and beta.dtype is _F32 and dgamma.dtype is _F32 and
+                 dbeta.dtype is _F32)
+    except (AttributeError, IndexError):
+        plain = False
+    if plain:
+        pg, px, ps, pa, pb, pd, da, db = (g.data_ptr(), x.data_ptr(), st.data_ptr(), gamma.data_ptr(), beta.data_ptr(),
+                                          d.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr())
+    else:
+        gt, xt, dt = _described(desc)
+        pg, px, ps, pa, pb, pd, da, db = _typed((g, gt, "g"), (x, xt, "x"), (st, _F32, "st"), (gamma, _F32, "gamma"),
+                                                (beta, _F32, "beta"), (d, dt, "d"), (dgamma, _F32, "dgamma"),
+                                                (dbeta, _F32, "dbeta"))
+    if workspace_bytes:
+        workspace_bytes = _nbytes(workspace_bytes)
+    _check(_lib.op_gn_backward(desc, pg, px, ps, pa, pb, drop, pd, da, db, _addr(workspace), workspace_bytes,
+                               _s(stream)))
 
 
 def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, ldr=0, ldy=0, stream=None):
@@ -736,5 +793,17 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
         xtype = _type_or(x, TYPE_BF16)
     if ytype is None:
         ytype = _type_or(y, xtype)
-    _check(_lib.op_dropout(rows, cols, xtype, _typed(x, xtype, "x"), ldx, _typed(res, ytype, "res"), ldr, ytype,
-                           _typed(y, ytype, "y"), ldy, drop, _s(stream)))
+    if (rows | cols | ldx | ldr | ldy) >> 62:
+        _fit("op_dropout", 62, rows, cols, ldx, ldr, ldy)
+    try:
+        yt = _DTYPES[ytype]
+        plain = x.dtype is _DTYPES[xtype] and y.dtype is yt and (res is None or res.dtype is yt)
+    except (AttributeError, IndexError):
+        plain = False
+    if plain:
+        px, pr, py = x.data_ptr(), res if res is None else res.data_ptr(), y.data_ptr()
+    else:
+        _fit("op_dropout: types", 31, xtype, ytype, large=E_INVALID)
+        yt = _TYPE_NAMES.get(ytype)
+        px, pr, py = _typed((x, _TYPE_NAMES.get(xtype), "x"), (res, yt, "res"), (y, yt, "y"))
+    _check(_lib.op_dropout(rows, cols, xtype, px, ldx, pr, ldr, ytype, py, ldy, drop, _s(stream)))

@@ -121,3 +121,37 @@ def test_generator_state_is_two_words_of_64_bits(rng):
     with pytest.raises(K.CkptError) as e:
         K.dropout(rng, 0.1)
     assert e.value.code == K.E_INVALID
+
+
+# ---------------------------------------------------- fields of fixed width --
+@pytest.mark.parametrize("kw", [dict(n=2 - (1 << 64)), dict(hw=-(1 << 64) + 1), dict(c=16 - (1 << 32)),
+                                dict(groups=4 - (1 << 32)), dict(act=1 << 32), dict(act=2 - (1 << 32)),
+                                dict(xtype=(1 << 32) + 1), dict(gtype=1 << 32), dict(dtype=-(1 << 32)),
+                                dict(ldx=16 - (1 << 64)), dict(ldd=1 << 64)])
+def test_descriptor_values_do_not_wrap(kw):
+    """Values that a narrower field would turn into valid ones."""
+    a = dict(n=2, hw=4, c=16, groups=4)
+    a.update(kw)
+    with pytest.raises(K.CkptError) as e:
+        K.gn_desc(**a)
+    assert e.value.code in (K.E_INVALID, K.E_UNSUPPORTED)
+
+
+@pytest.mark.parametrize("rows,cols,kw", [((1 << 64) + 4, 8, {}), (4 - (1 << 64), 8, {}), (4, (1 << 64) + 8, {}),
+                                          (4, 8, dict(ldx=1 << 64)), (4, 8, dict(ldr=8 - (1 << 64))),
+                                          (4, 8, dict(ldy=1 << 65)), (4, 8, dict(xtype=1 << 32)),
+                                          (4, 8, dict(ytype=(1 << 32) + 1))])
+def test_dropout_sizes_do_not_wrap(lib, rows, cols, kw):
+    with pytest.raises(K.CkptError) as e:
+        K.op_dropout(rows, cols, 4096, 8192, drop(), **kw)
+    assert e.value.code in (K.E_INVALID, K.E_UNSUPPORTED) and not lib.calls
+
+
+@pytest.mark.parametrize("nbytes", [-1, 16 - (1 << 64), 1 << 64])
+def test_workspace_sizes_do_not_wrap(lib, nbytes):
+    d = K.gn_desc(2, 1 << 20, 16, 4)
+    for call in (lambda: K.op_gn_forward(d, *(4096,) * 5, 4096, nbytes),
+                 lambda: K.op_gn_backward(d, *(4096,) * 8, 4096, nbytes)):
+        with pytest.raises(K.CkptError) as e:
+            call()
+        assert e.value.code == K.E_INVALID and not lib.calls
