@@ -8,8 +8,9 @@
 // arguments must lie inside one of those allocations (or the library's static
 // scratch); the bf16 GEMM's argument block is checked over the whole extent
 // each operand spans for the launch's shape, leading dimensions, operand forms,
-// gathers, epilogue and split count.  Grid and block sizes are checked
-// against the device limits.  Errors are counted and the first few printed.
+// gathers, epilogue and split count, and so are a group norm's tensors and the
+// records its launches leave.  Grid and block sizes are checked against the device
+// limits.  Errors are counted and the first few printed.
 #include <cxxabi.h>
 #include <hip/hip_runtime.h>
 
@@ -17,6 +18,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <iterator>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -24,6 +26,7 @@
 #include <vector>
 
 #include "../../paper_1604_06174_amd/csrc/gemm_bf16_kernel.h"
+#include "../../paper_1604_06174_amd/csrc/gn.h"
 #include "../../paper_1604_06174_amd/csrc/kernel_args.h"
 
 namespace {
@@ -37,7 +40,7 @@ struct Region {
 };
 
 struct Param {
-  enum Kind { PTR, SCALAR, GEMM_BF16, CONV, WGRAD, GEMM_F32 } kind;
+  enum Kind { PTR, SCALAR, GEMM_BF16, CONV, WGRAD, GEMM_F32, GN, DROPOUT } kind;
 };
 
 struct KernelInfo {
@@ -189,6 +192,9 @@ void parse(KernelInfo &k) {
     else if (t == "ckpt::ConvArgs") q.kind = Param::CONV;
     else if (t == "ckpt::WgArgs") q.kind = Param::WGRAD;
     else if (t == "ckpt::GemmArgs") q.kind = Param::GEMM_F32;
+    else if (t == "ckpt::GnArgs") q.kind = Param::GN;
+    else if (t == "ckpt::(anonymous namespace)::Args" && p.find("k_dropout<") != std::string::npos)
+      q.kind = Param::DROPOUT;
     else if (t == "int" || t == "long" || t == "unsigned int" || t == "unsigned long" || t == "float" ||
              t == "double" || t == "bool" || t == "long long" || t == "unsigned long long")
       q.kind = Param::SCALAR;
@@ -312,6 +318,42 @@ void check_gemm_bf16(const KernelInfo &k, const ckpt::gb::Args &a, dim3 grid) {
   }
 }
 
+// a group norm's tensors over their whole extent (types by the template arguments of
+// the kernels that take the tensors), its parameters and statistics, and the records of
+// channel sums a backward leaves and adds up
+void check_gn(const KernelInfo &k, const ckpt::GnArgs &a) {
+  const uint64_t C = uint64_t(a.C), pixels = uint64_t(a.n) * a.hw, ng = uint64_t(a.n) * a.G;
+  auto size = [&](size_t i) { return uint64_t(i < k.targs.size() && k.targs[i] == "float" ? 4 : 2); };
+  auto is = [&](const char *name) { return k.pretty.find(name) != std::string::npos; };
+  const bool bwd = is("k_gn_bwd<") || is("k_gn_bwd_sums<") || is("k_gn_bwd_apply<");
+  if (bwd || is("k_gn_fwd<") || is("k_gn_stats<") || is("k_gn_apply<") || is("k_gn_apply_rows<"))
+    check_extent(k, "x", a.x, rows_span(pixels, a.ldx, C) * size(0));
+  if (bwd) check_extent(k, "g", a.g, rows_span(pixels, a.ldg, C) * size(1));
+  if (is("k_gn_bwd<") || is("k_gn_bwd_apply<")) check_extent(k, "d", a.out, rows_span(pixels, a.ldo, C) * size(2));
+  if (is("k_gn_fwd<") || is("k_gn_apply<") || is("k_gn_apply_rows<"))
+    check_extent(k, "y", a.out, rows_span(pixels, a.ldo, C) * size(0));
+  if (!is("k_gn_records")) {
+    check_extent(k, "gamma", a.gamma, C * 4);
+    check_extent(k, "beta", a.beta, C * 4);
+    check_extent(k, "statistics", a.st, 2 * ng * 4);
+  }
+  if (is("k_gn_stats<")) check_extent(k, "chunks", a.gpart, ng * a.chunks * 8);
+  if (is("k_gn_merge(") || is("k_gn_apply<") && k.targs.size() > 2 && k.targs[2] == "true")
+    check_extent(k, "chunks", a.gpart, ng * a.chunks1 * 8);
+  if (is("k_gn_bwd_sums<")) check_extent(k, "records", a.cpart, uint64_t(a.n) * a.chunks * 2 * C * 4);
+  if (is("k_gn_bwd_apply<") || is("k_gn_bwd_merge("))
+    check_extent(k, "records", a.cpart, uint64_t(a.n) * a.chunks1 * 2 * C * 4);
+  if (is("k_gn_records(") || is("k_gn_bwd<") && a.cpart)
+    check_extent(k, "records", a.cpart, uint64_t(a.rows) * 2 * C * 4);
+  if (is("k_gn_bwd<") && !a.cpart && a.rows > 1) error(k.pretty + ": several records and no place for them");
+  if (is("k_gn_bwd_merge(") || is("k_gn_bwd_apply<") && a.gsum) check_extent(k, "group sums", a.gsum, ng * 8);
+  if (bwd) {
+    check_extent(k, "dgamma", a.dgamma, C * 4);
+    check_extent(k, "dbeta", a.dbeta, C * 4);
+  }
+  if (a.drop.rng) check_extent(k, "seed and step", a.drop.rng, 16);
+}
+
 void check_launch(const void *f, dim3 grid, dim3 block, void **args, size_t shm) {
   std::lock_guard<std::mutex> lock(S().mu);
   ++S().launches;
@@ -353,6 +395,11 @@ void check_launch(const void *f, dim3 grid, dim3 block, void **args, size_t shm)
         for (const void *q : ps) check_ptr(k, "GemmArgs field", q);
         break;
       }
+      case Param::GN: check_gn(k, *static_cast<const ckpt::GnArgs *>(args[i])); break;
+      case Param::DROPOUT: {  // three tensors first
+        for (int q = 0; q < 3; ++q) check_ptr(k, "a dropout tensor", static_cast<void *const *>(args[i])[q]);
+        break;
+      }
       case Param::SCALAR: break;
     }
   }
@@ -392,6 +439,16 @@ void hc_counters(uint64_t *launches, uint64_t *errors, uint64_t *ptr_checks, uin
   *errors = S().errors;
   *ptr_checks = S().ptr_checks;
   *extent_checks = S().extent_checks;
+}
+
+// the i-th kernel's mangled name (null past the last) and how often it was launched
+const char *hc_kernel(uint64_t i, uint64_t *launches) {
+  std::lock_guard<std::mutex> lock(S().mu);
+  if (i >= S().kernels.size()) return nullptr;
+  auto it = S().kernels.begin();
+  std::advance(it, i);
+  *launches = it->second.launches;
+  return it->second.mangled.c_str();
 }
 
 // ---- registration (called by the host-only objects' static constructors) --
