@@ -719,7 +719,9 @@ typedef struct ckpt_gn_desc {
 
 /* op_gn_workspace_bytes -- device workspace op_gn_forward (backward = 0) or
  * op_gn_backward needs for this problem, 0 for none (a null workspace
- * will do).  Calls that share one must not overlap.
+ * will do).  Calls that share one must not overlap.  A backward keeps channel sums,
+ * 8 c bytes for each of its workgroups: 17 MB at most for samples of up to four pixels
+ * (two where the channels are taken one by one), else less than the tensor takes in fp32.
  * Errors: CKPT_E_INVALID for sizes below 1, groups that do not divide c, an
  * unknown activation or type, a stride below c, eps <= 0; CKPT_E_UNSUPPORTED
  * for n hw c >= 2^35, n hw >= 2^30, n groups >= 2^25, c > 2^20, or more than

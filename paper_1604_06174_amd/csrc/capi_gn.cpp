@@ -108,6 +108,8 @@ ckpt::GnPlan plan_of(const ckpt::GnProblem &p, bool backward, const void *worksp
   const ckpt::GnPlan g = ckpt::gn_plan(p, backward);
   grid_fits(g.first, fn);
   grid_fits(g.second, fn);
+  // what a forward of the same samples would be refused for (a backward's may loop)
+  if (g.resident && !g.wave && p.n * g.first.tiles >= (int64_t(1) << 21)) refuse(CKPT_E_UNSUPPORTED, fn, ": tensor too large");
   const uint64_t want = ckpt::gn_workspace_bytes(g);
   if (want) {
     need_ptr(workspace, fn, "workspace", 16);

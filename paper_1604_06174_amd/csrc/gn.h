@@ -45,8 +45,9 @@ enum { GN_RED_TREE = 0, GN_RED_COLUMNS = 1, GN_RED_GROUPS = 2 };
 // The passes of a call.
 struct GnPlan {
   // resident: a sample's tile (whole groups) stays in the registers of one team, NV
-  // vectors a thread; `wave`: of one wavefront each, `teams` a workgroup (else the
-  // workgroup is the team, its samples' `rows` records of channel sums)
+  // vectors a thread; `wave`: of one wavefront each, `teams` a workgroup, else the
+  // workgroup is the team.  `rows` workgroups a tile, each with a record of channel sums:
+  // below n they loop over samples
   bool resident, wave;
   int NV, teams;
   int pack;  // samples of one pixel that a wavefront takes at once (1: its rows are pixels)

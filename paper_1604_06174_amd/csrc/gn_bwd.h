@@ -85,19 +85,26 @@ __device__ __forceinline__ void channel_record(const GnArgs &A, const Team<WAVE>
   }
 }
 
+// Resident teams: a workgroup with one sample, a wavefront that loops over samples,
+// and a workgroup that does (gn_plan: more samples than fill the device).
+enum { GNB_ONE = 0, GNB_WAVE = 1, GNB_LOOP = 2 };
+
 // Wavefronts a SIMD that a resident kernel's registers leave room for: 4 (128
-// registers), 2 where its vectors, or the sums of eight channels that a wavefront
-// keeps from sample to sample, take more (2048 samples of 16 pixels x 64 channels in
+// registers), 2 where its vectors, or the sums of eight channels that a team keeps from
+// sample to sample, take more (wavefronts, 2048 samples of 16 pixels x 64 channels in
 // groups of four: 17.1 us held to 128 registers, 11.9 not).
-template <int V, int NV, int NJ, bool WAVE>
+template <int V, int NV, int NJ, int TEAM>
 constexpr int gnb_waves() {
-  return V == 8 && (NV >= 4 || (WAVE && NJ > 1)) ? 2 : 4;
+  return V == 8 && (NV >= 4 || (TEAM != GNB_ONE && NJ > 1) || (TEAM == GNB_LOOP && NV >= 2)) ? 2 : 4;
 }
 
-// Resident: one team per (sample, tile); a wavefront's loops over samples.
-template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, bool WAVE, int RED, bool SILU,
+// Resident: one team per (sample, tile), or per tile of several samples in turn.
+// GNB_LOOP chooses SiLU and dropout as it runs (from its second sample on, the code
+// jumped to is in the instruction cache), the others are compiled for them.
+template <typename XT, typename GT_, typename DT, int V, int NV, int NJ, int TEAM, int RED, bool SILU,
           bool DROP>
-__global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, (gnb_waves<V, NV, NJ, WAVE>())) void k_gn_bwd(GnArgs A) {
+__global__ __launch_bounds__(TEAM == GNB_WAVE ? 256 : V == 8 ? 512 : 1024, (gnb_waves<V, NV, NJ, TEAM>())) void k_gn_bwd(GnArgs A) {
+  constexpr bool WAVE = TEAM == GNB_WAVE;
   extern __shared__ float lds[];
   const Team<WAVE> tm(A);
   const int teams = WAVE ? blockDim.x / 64 : 1;
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, (gnb_waves<V, NV,
   // a wavefront's rows are pixels, or samples of one
   const bool packed = WAVE && A.pack > 1;
   const int ty = packed ? 0 : tm.ty, step = A.rows * teams * (WAVE ? A.pack : 1);
-  for (int i0 = (by * teams + tm.index) * (WAVE ? A.pack : 1); i0 < A.n; i0 = WAVE ? i0 + step : A.n) {
+  for (int i0 = (by * teams + tm.index) * (WAVE ? A.pack : 1); i0 < A.n; i0 = TEAM == GNB_ONE ? A.n : i0 + step) {
     const bool live = !packed || i0 + tm.ty < A.n, col = column && live && ty < A.TY;
     const int i = packed ? min(i0 + tm.ty, A.n - 1) : i0;
     const int64_t pix0 = int64_t(i) * A.hw;
@@ -150,7 +157,11 @@ __global__ __launch_bounds__(WAVE ? 256 : V == 8 ? 512 : 1024, (gnb_waves<V, NV,
       if (col && ty + k * A.TY < A.hw) {
 #pragma unroll
         for (int j = 0; j < V; ++j) du[k][j] = float(gr[k].v[j]);
-        cp.template du<SILU, DROP>(A, key, xr[k], uint64_t(pix0 + ty + k * A.TY), c, du[k]);
+        const uint64_t pix = uint64_t(pix0 + ty + k * A.TY);
+        if constexpr (TEAM == GNB_LOOP)
+          gn_choose(A, [&](auto silu, auto drop) { cp.template du<silu.value, drop.value>(A, key, xr[k], pix, c, du[k]); });
+        else
+          cp.template du<SILU, DROP>(A, key, xr[k], pix, c, du[k]);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           s1[j] += du[k][j];
@@ -298,16 +309,26 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
 }
 
 // dgamma | dbeta from `rows` records [2][C]: the 16 columns from 16 blk, a thread
-// per column and row in turn, added in a fixed order.  red: [blockDim / 16][17].
+// per column and row in turn, added in a fixed order.  A call of many samples may have
+// a record for each: they are taken eight at a time without conditions (with one per load
+// these waited for each other: the sums of 20000 records of 64 channels 55 us, now 33) and
+// added as a tree.  red: [blockDim / 16][17].
 __device__ __forceinline__ void record_sums(const GnArgs &A, int rows, int blk, float *red) {
   const int e = blk * 16 + threadIdx.x % 16, r0 = threadIdx.x / 16, R = blockDim.x / 16;
   float s = 0.f;
   if (e < 2 * A.C) {
+    const float *const part = A.cpart + e;
     constexpr int U = 8;
-    for (int r = r0; r < rows; r += U * R) {
-      float v[U];
+    float v[U];
+    int r = r0;
+    for (; r + (U - 1) * R < rows; r += U * R) {
 #pragma unroll
-      for (int k = 0; k < U; ++k) v[k] = r + k * R < rows ? A.cpart[int64_t(r + k * R) * 2 * A.C + e] : 0.f;
+      for (int k = 0; k < U; ++k) v[k] = part[int64_t(r + k * R) * 2 * A.C];
+      s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
+    if (r < rows) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) v[k] = r + k * R < rows ? part[int64_t(r + k * R) * 2 * A.C] : 0.f;
 #pragma unroll
       for (int k = 0; k < U; ++k) s += v[k];
     }
@@ -464,11 +485,22 @@ void launch_resident(hipStream_t s, const GnPlan &g, const GnArgs &a) {
     // a wavefront's tile ends at two vectors a thread (gn_plan)
     if constexpr (NV <= 2)
       if (g.wave)
-        return g.red == GN_RED_GROUPS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, GN_RED_GROUPS, S, D>)
-                                      : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, true, GN_RED_COLUMNS, S, D>);
-    g.red == GN_RED_GROUPS    ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_GROUPS, S, D>)
-    : g.red == GN_RED_COLUMNS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_COLUMNS, S, D>)
-                              : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, false, GN_RED_TREE, S, D>);
+        return g.red == GN_RED_GROUPS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_WAVE, GN_RED_GROUPS, S, D>)
+                                      : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_WAVE, GN_RED_COLUMNS, S, D>);
+    // a workgroup loops over samples of four pixels at most, or two (gn_plan); 64 columns
+    // or fewer it takes only with three or four, two a thread
+    if constexpr (NV <= (V == 8 ? 4 : 2))
+      if (g.rows < a.n) {
+        if constexpr (V == 8 && NV == 2) {
+          if (g.red == GN_RED_COLUMNS) return go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_LOOP, GN_RED_COLUMNS, false, false>);
+          if constexpr (NJ == 1)
+            if (g.red == GN_RED_GROUPS) return go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_LOOP, GN_RED_GROUPS, false, false>);
+        }
+        return go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_LOOP, GN_RED_TREE, false, false>);
+      }
+    g.red == GN_RED_GROUPS    ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_ONE, GN_RED_GROUPS, S, D>)
+    : g.red == GN_RED_COLUMNS ? go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_ONE, GN_RED_COLUMNS, S, D>)
+                              : go(k_gn_bwd<XT, GT_, DT, V, NV, NJ, GNB_ONE, GN_RED_TREE, S, D>);
   });
 }
 

@@ -156,6 +156,19 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
       g.resident = true;
       g.NV = int(nv);
       g.rows = p.n;
+      // a backward's workgroups loop over samples of so few pixels that a record of channel
+      // sums for each (8 bytes a channel) would outweigh the sample: as many of them as the
+      // device holds at once, 1024 at most (microseconds, a record per sample and this way:
+      // 16384 rows of 1024 channels 115 and 41, 2048 of them 20 and 16, 4000 samples of 2 x
+      // 4096 113 and 72, 8000 of 4 x 512 51 and 35; of 8 pixels some sizes lose: 8000 x 504
+      // channels in twelves 77 and 84; element by element 8000 of 2 x 515 58 and 36, with
+      // SiLU and dropout 77 and 60, of 3 pixels 91 and 112), and two samples each where
+      // the records would take 12 MB (1000 rows of 2048 17.6 and 15.8, 500 of 4096 18.1 and
+      // 15.8; of 10 MB and less some lose: 400 samples of 4 x 3000 17.8 and 18.3)
+      if (backward && p.hw <= (v.V == 8 ? 4 : 2)) {
+        const int64_t held = std::max(1, std::min(1024, (1 << 18) / v.threads) / v.tiles);
+        g.rows = std::min(held, p.n * p.C >= (3 << 19) ? ceil_div(p.n, 2) : p.n);
+      }
     }
   }
   if (g.resident) {
