@@ -339,21 +339,35 @@ __device__ __forceinline__ float gn_affine(float x, float mean, float a, float b
   return m + b;
 }
 
-__device__ __forceinline__ float gn_sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __expf(-u)); }
+// e^-u for fp32 activations, two steps off at most: 2^t with t the rounded product of -u
+// and log2 e, times 1 + ln 2 (what the product's rounding and the constant's left).
+// Past 200 either way it is 0 or infinite (there infinities would meet in that rest).
+__device__ __forceinline__ float gn_exp_neg(float u) {
+  const float v = __builtin_amdgcn_fmed3f(-u, -200.f, 200.f);
+  const float t = v * 1.44269502f, rest = fmaf(v, 1.92596303e-8f, fmaf(v, 1.44269502f, -t));
+  return __builtin_amdgcn_exp2f(t) * fmaf(rest, 0.693147181f, 1.f);
+}
+
+// FINE: fp32 activations.  bf16 ones take the exponential in two instructions: its
+// relative error, |u| half steps of fp32 below zero, is a ten-thousandth of their own.
+template <bool FINE>
+__device__ __forceinline__ float gn_sigmoid(float u) {
+  return __builtin_amdgcn_rcpf(1.f + (FINE ? gn_exp_neg(u) : __expf(-u)));
+}
 
 // v = act(u), not SiLU: ReLU (NaN passes through) or nothing by a uniform flag, which
 // costs no jump
-template <bool SILU>
+template <bool SILU, bool FINE>
 __device__ __forceinline__ float gn_act(bool relu, float u) {
-  if (SILU) return u * gn_sigmoid(u);
+  if (SILU) return u * gn_sigmoid<FINE>(u);
   return relu && u < 0.f ? 0.f : u;
 }
 
 // dv act'(u)
-template <bool SILU>
+template <bool SILU, bool FINE>
 __device__ __forceinline__ float gn_act_bwd(bool relu, float u, float dv) {
   if (SILU) {
-    const float q = gn_sigmoid(u);
+    const float q = gn_sigmoid<FINE>(u);
     return dv * (q * (1.f + u * (1.f - q)));
   }
   return u > 0.f || !relu ? dv : 0.f;

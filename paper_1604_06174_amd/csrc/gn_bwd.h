@@ -35,7 +35,7 @@ struct Column {
     if (SILU || A.act == GN_ACT_RELU)
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        g[j] = gn_act_bwd<SILU>(true, gn_affine(float(x.v[j]), mean[NJ == 1 ? 0 : j], a[j], beta[j]), g[j]);
+        g[j] = gn_act_bwd<SILU, sizeof(XT) == 4>(true, gn_affine(float(x.v[j]), mean[NJ == 1 ? 0 : j], a[j], beta[j]), g[j]);
   }
   template <typename DT>
   __device__ __forceinline__ void put(const GnArgs &A, const Vec<XT, V> &x, const float (&k1)[NJ],

@@ -24,7 +24,7 @@ struct Column {
   __device__ __forceinline__ void put(const GnArgs &A, const DropKey &key, const Vec<XT, V> &x, int64_t pix, int c) const {
     float v[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = gn_act<SILU>(A.act == GN_ACT_RELU, gn_affine(float(x.v[j]), mean[NJ == 1 ? 0 : j], a[j], b[j]));
+    for (int j = 0; j < V; ++j) v[j] = gn_act<SILU, sizeof(XT) == 4>(A.act == GN_ACT_RELU, gn_affine(float(x.v[j]), mean[NJ == 1 ? 0 : j], a[j], b[j]));
     if (DROP) gn_drop<V>(A, key, uint64_t(pix), c, v);
     store_vec<XT, V>(static_cast<XT *>(A.out) + pix * A.ldo + c, v);
   }

@@ -1,11 +1,11 @@
 """Accuracy of group norm where its range makes it hard: a first value far from
-the others.  Bars are worst cases of the fp32 operations, counted beside each test.
+the others, SiLU far below zero.  Bars are worst cases of the fp32 operations, counted beside each test.
 """
 import numpy as np
 import pytest
 
 from oracle import norm as N
-from test_gpu_gn import DEV, EPS, L, _K, host, rounded, torch, types
+from test_gpu_gn import DEV, EPS, L, _K, f32, host, rounded, torch, types
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +65,67 @@ def test_statistics_with_an_outlying_first_value(shape, x):
     absmean = np.abs(base.astype(np.float64)).reshape(8, hw, groups, -1).mean((1, 3))
     assert (np.abs(s[0] - mean) <= U * np.abs(mean) + L * absmean).all()
     assert (err <= 320 * U).all()
+
+
+# ------------------------------------------------------------------- SiLU --
+def _levels():
+    """u from -80 (where silu' = u e^u is still a normal number) to 80."""
+    rng = np.random.default_rng(45)
+    u = np.concatenate([np.linspace(-80, 80, 4001), rng.uniform(-80, 0, 4000), rng.uniform(-2, 2, 2000), [0.0]])
+    return u.astype(np.float32)
+
+
+def _identity(u, dt):
+    """Statistics, scale and shift that make u of a bf16 or fp32 x exactly x."""
+    c = u.size
+    K = _K()
+    code = {torch.float32: K.TYPE_F32, torch.bfloat16: K.TYPE_BF16}[dt]
+    d = K.gn_desc(1, 1, c, c, act=K.ACT_SILU, xtype=code, gtype=K.TYPE_F32, dtype=K.TYPE_F32)
+    st = f32(np.concatenate([np.zeros(c), np.ones(c)]))
+    return d, torch.from_numpy(u).to(DEV).to(dt).view(1, c), st, torch.ones(c, device=DEV), torch.zeros(c, device=DEV)
+
+
+def _pad8(u, n):
+    return u[:u.size // 8 * 8] if n == 8 else u[:u.size // 8 * 8 - 1]
+
+
+@pytest.mark.parametrize("vec", [8, 1])
+def test_silu_of_fp32(vec):
+    """x sigmoid(x) relative to itself: the exponential (a step and a half at most),
+    the sum, the reciprocal (a step) and the product are below 8 half steps."""
+    K = _K()
+    print(f"[gn silu] {vec}", flush=True)
+    u = _pad8(_levels(), vec)
+    d, x, st, ga, be = _identity(u, torch.float32)
+    y = torch.empty_like(x)
+    K.op_gn_apply(d, x, st, ga, be, y)
+    want = u.astype(np.float64) * N.sigmoid(u.astype(np.float64))
+    err = np.abs(host(y).reshape(-1) - want)
+    print(f"    {np.max(err[want != 0] / np.abs(want[want != 0])) / U:.1f} half steps", flush=True)
+    assert (err <= 8 * U * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("vec", [8, 1])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_silu_slope(vec, x):
+    """The shift's gradient of a single pixel is g silu'(u) itself: q (1 + u (1 - q))
+    with q = sigmoid(u) to 6 half steps, three operations more and the product with g,
+    relative to q (1 + |u| (1 - q)); 1 - q to four half steps of 1.  A bf16 x takes the
+    exponential whose relative error is 1.25 |u| half steps and two more."""
+    K = _K()
+    print(f"[gn silu'] {vec} {x}", flush=True)
+    u = _pad8(rounded(_levels(), x), vec)
+    d, xd, st, ga, be = _identity(u, torch.float32 if x == "f32" else torch.bfloat16)
+    g = np.random.default_rng(46).standard_normal(u.size).astype(np.float32)
+    dx, dg, db = torch.empty(1, u.size, device=DEV), torch.empty(u.size, device=DEV), torch.empty(u.size, device=DEV)
+    nb = K.op_gn_workspace_bytes(d, True)
+    ws = torch.empty(max(16, nb), dtype=torch.uint8, device=DEV)
+    K.op_gn_backward(d, f32(g).view(1, -1), xd, st, ga, be, dx, dg, db, ws, nb)
+    w = u.astype(np.float64)
+    q = N.sigmoid(w)
+    want = g * (q * (1 + w * (1 - q)))
+    steps = 24.0 if x == "f32" else 24.0 + 2 * (1.25 * np.abs(w) + 2)
+    bar = U * np.abs(g) * q * (steps * (1 + np.abs(w) * (1 - q)) + 4 * np.abs(w))
+    err = np.abs(host(db) - want)
+    print(f"    {np.max(err / (bar + 1e-37)):.3f} of its bar", flush=True)
+    assert (err <= bar + 1e-37).all()
