@@ -1,11 +1,12 @@
 """Accuracy of group norm where its range makes it hard: a first value far from
-the others, SiLU far below zero.  Bars are worst cases of the fp32 operations, counted beside each test.
+the others, a mean far from zero, SiLU far below zero.  Bars are worst cases of
+the fp32 operations, counted beside each test.
 """
 import numpy as np
 import pytest
 
 from oracle import norm as N
-from test_gpu_gn import DEV, EPS, L, _K, f32, host, rounded, torch, types
+from test_gpu_gn import DEV, EPS, L, Case, _K, f32, host, rounded, torch, types
 
 pytestmark = pytest.mark.gpu
 
@@ -65,6 +66,50 @@ def test_statistics_with_an_outlying_first_value(shape, x):
     absmean = np.abs(base.astype(np.float64)).reshape(8, hw, groups, -1).mean((1, 3))
     assert (np.abs(s[0] - mean) <= U * np.abs(mean) + L * absmean).all()
     assert (err <= 320 * U).all()
+
+
+# ------------------------------------------------- a mean far from zero ------
+FAR_SHAPES = {
+    "rows": (300, 1, 1024, 16),
+    "rows_packed": (4100, 1, 64, 4),
+    "layer_rows": (1500, 1, 1024, 1),
+    "layer_rows_fours": (700, 1, 1000, 2),
+    "wave_two_vectors": (2048, 16, 64, 8),
+    "wave_fours": (2048, 16, 64, 16),
+    "resident": (32, 196, 256, 32),
+    "resident_odd_groups": (5, 100, 120, 12),
+    "resident_eight_vectors": (64, 784, 64, 8),
+    "split": (2, 3136, 64, 32),
+    "split_many_chunks": (1, 40000, 64, 8),
+    "split_odd_groups": (3, 2777, 72, 6),
+    "scalar": (7, 65, 37, 37),
+    "scalar_rows": (1500, 1, 515, 5),
+    "scalar_split": (2, 9001, 6, 2),
+}
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", list(FAR_SHAPES))
+def test_one_offset_for_all_values(shape, x):
+    """A spread of one on a level of a thousand (bf16: of 64, where its steps are
+    still a quarter of the spread) that all channels share.  1 / std from the squares
+    of the differences: L for the sums, and the square of the mean's error in
+    standard deviations; a difference of the squares' mean and the mean's square is
+    off by a hundred times that."""
+    level = 1000.0 if x == "f32" else 64.0
+    print(f"[gn far] {shape} {x}", flush=True)
+    c = Case(*FAR_SHAPES[shape], x=x, level=0.0, seed=43)
+    v = rounded(np.random.default_rng(44).standard_normal(c.xv.shape) + level, x)
+    c.xv, c.x3 = v, v.reshape(c.n, c.hw, c.c)
+    c.X.m.copy_(torch.from_numpy(v))
+    mean, rstd = N.group_stats(c.x3, c.groups, EPS)
+    # the groups have eight values or more
+    assert (1 / (rstd * mean)).max() <= (3e-3 if x == "f32" else 5e-2)
+    s = host(c.check_forward()).reshape(2, c.n, c.groups)
+    off = np.abs(s[1] / rstd - 1)
+    bar = U + L + (L * mean * rstd) ** 2
+    print(f"    1 / std: {(off / bar).max():.3f} of its bar", flush=True)
+    assert (off <= bar).all()
 
 
 # ------------------------------------------------------------------- SiLU --

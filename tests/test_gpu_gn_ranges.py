@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 import gn_cases as R
+import test_gpu_gn as B
 from oracle import norm as N
 from test_gpu_gn import DEV, Case, _K, f32, host, torch
 
@@ -41,6 +42,33 @@ def test_many_samples(shape, x):
         if i == 0:
             c.check_forward()
         c.check_backward()
+
+
+# teams that the shapes of these checks in test_gpu_gn.py leave out
+TEAMS = {
+    "wave_two_vectors": (2048, 16, 64, 8),
+    "wave_fours": (2048, 16, 64, 16),
+    "wave_padded": (1039, 9, 40, 4),
+    "wave_packed": (4100, 1, 64, 4),
+    "wave_packed_fours": (2101, 1, 32, 8),
+    "loop_rows": (1203, 1, 2048, 2),
+    "loop_rows_halves": (2300, 1, 1000, 2),
+    "loop_rows_s": (1203, 2, 1030, 2),
+    "loop_four_pixels": (1301, 4, 1024, 2),
+    "resident_sixteen_vectors": (66, 130, 264, 8),
+}
+
+
+@pytest.mark.parametrize("shape", list(TEAMS))
+def test_special_values_stay_in_their_group(shape, monkeypatch):
+    monkeypatch.setitem(B.SHAPES, shape, TEAMS[shape])
+    B.test_special_values_stay_in_their_group(shape)
+
+
+@pytest.mark.parametrize("shape", list(TEAMS))
+def test_same_bits_and_in_place(shape, monkeypatch):
+    monkeypatch.setitem(B.SHAPES, shape, TEAMS[shape])
+    B.test_same_bits_and_in_place(shape)
 
 
 def _wide(rows, ld, dtype):
