@@ -726,9 +726,10 @@ typedef struct ckpt_gn_desc {
  * Errors: CKPT_E_INVALID for sizes below 1, groups that do not divide c, an
  * unknown activation or type, a stride below c, eps <= 0; CKPT_E_UNSUPPORTED
  * for n hw c >= 2^35, n hw >= 2^30, n groups >= 2^25, c > 2^20, or more than
- * 1024 channels per group (up to 4096 are served where 8 divides them); the
- * calls also refuse what would take 2^21 workgroups (two million samples of
- * more pixels than a wavefront covers at once). */
+ * 1024 channels per group (up to 4096 are served where 8 divides them, up to
+ * 2048 where 4 does and 8 divides c); the calls also refuse what would take 2^21 workgroups: samples times tiles of 64 channels
+ * (32 of fp32; more where groups are wider or pixels few) where a wavefront does not
+ * hold a sample's tile. */
 int op_gn_workspace_bytes(const ckpt_gn_desc *desc, int32_t backward, uint64_t *bytes);
 
 /*

@@ -232,7 +232,7 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
   const XT *const x = static_cast<const XT *>(A.x) + pix0 * A.ldx + c;
   const GT_ *const g = static_cast<const GT_ *>(A.g) + pix0 * A.ldg + c;
   // vectors in flight besides those worked on: more cost registers that hide the
-  // arithmetic better (stage 1 with dropout: 59 us, 62 with two)
+  // arithmetic better (stage 1 with dropout: 58.6 us, 61.9 with two)
   constexpr int U = V == 1 ? 4 : 1;
   Vec<XT, V> xr[U];
   Vec<GT_, V> gr[U];
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
     gn_choose(A, [&](auto silu, auto drop) {
       int r = tm.ty;
       // element by element, while every thread has all its pixels (k_gn_apply; vectors
-      // lose by it, their time is arithmetic: stage 1 with dropout 59 -> 64 us)
+      // lose by it: stage 1 with dropout 58.6 -> 62.7 us)
       for (int q = 2 * U * A.TY; V == 1 && q <= np; q += U * A.TY, r += U * A.TY) {
         Vec<XT, V> nx[U];
         Vec<GT_, V> ng[U];

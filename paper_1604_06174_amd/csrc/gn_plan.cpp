@@ -92,7 +92,7 @@ GnCover gn_cover_elements(const GnProblem &p, int V, bool whole_groups) {
   v.TY = int(std::min<int64_t>(v.TY, p.hw));
   v.threads = int(up(int64_t(v.TY) * v.VC, 64));
   // four workgroups a CU, one turn: each forms its channels' parameters once (the stem's
-  // forward: 33 us, 35 at 2048, 47 at 4096)
+  // forward: 32.2 us, 32.7 at 2048, 33.9 at 4096)
   cut(p, 1024, 4, v);
   return v;
 }
@@ -143,7 +143,7 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
     if (backward) g.rows = std::min(g.rows, std::max<int64_t>(std::min<int64_t>(turns, 64), ceil_div(turns, 2)));
   } else {
     // two vectors a thread while the workgroup may grow (one sample of 49 pixels x 512
-    // channels, forward: 3.9 us; at four vectors 4.6, at eight 5.8)
+    // channels, forward: 3.7 us; at four vectors 4.5, at eight 5.7)
     v.threads = int(std::min<int64_t>(cap, up(v.VC * ceil_div(p.hw, 2), 64)));
     if (v.threads < v.VC) v.threads = int(up(v.VC, 64));
     v.TY = v.threads / v.VC;
@@ -151,7 +151,9 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
     // few slabs only while one is read in a few microseconds by its one compute unit
     // (bf16 forward, microseconds resident and split: 4 slabs of 3200 vectors 7.4 and
     // 8.7, of 6272 vectors 10.7 and 8.8; 32 of them 11.1 and 9.6, 64 11.9 and 12.4; 256
-    // 20.0 and 24.8)
+    // 20.0 and 24.8).  fp32 and the backward follow: 16 to 512 slabs of up to 3200 vectors
+    // all lose by splitting (64 of 3200, bf16 backward 10.1 and 10.5, 512 of them 24.0 and
+    // 26.3; of 1600 fp32 ones forward 8.1 and 9.6, backward 10.3 and 11.5)
     if (nv <= nv_max && (slabs >= 64 || vecs <= 4096)) {
       g.resident = true;
       g.NV = int(nv);
@@ -180,19 +182,20 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
   v.threads = int(std::max<int64_t>(256, up(v.VC, 64)));
   v.TY = v.threads / v.VC;
   // two workgroups a CU: fewer chunks to add up outweigh the latency that four would
-  // hide (stage-1 backward with dropout: 61 us, 64 at 1024)
+  // hide (stage-1 backward with dropout: 58.6 us, 60.1 at 1024, 66.0 at 256)
   cut(p, 512, 4, v);
   reductions(p, backward, backward ? 0 : 1, g);
   if (backward) {
     // adding up the chunks costs every workgroup of the second pass more the more there
-    // are (196 of them: 27.7 us, 17.5 with a launch for it; 49: 13.7 and 12.5), and
-    // groups wider than a tile have to be formed outside
+    // are (a sample of 50176 pixels x 64 channels, 392 chunks: 27.6 us, 16.9 with a launch
+    // for it; four of them, 121 chunks each: 32.7 and 31.2), and groups wider than a tile
+    // have to be formed outside
     g.merge = v.chunks > 32 || p.cg > 64;
     g.ws_channels = align256(uint64_t(p.n) * v.chunks * 2 * p.C * 4);
     if (g.merge) g.ws_sums = align256(uint64_t(p.n) * p.G * 8);
   } else {
-    // (98 chunks: 13.1 us in the second pass, 10.2 with a launch; 64 or fewer are read at
-    // once)
+    // (392 chunks: 29.5 us, 14.7 with a launch; 98: 13.3 and 10.4; 64 or fewer are read
+    // at once)
     g.merge = v.chunks > 64;
     g.ws_groups = align256(uint64_t(p.n) * v.chunks * p.G * 8);
   }
