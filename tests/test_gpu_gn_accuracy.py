@@ -1,6 +1,6 @@
 """Accuracy of group norm where its range makes it hard: a first value far from
-the others, a mean far from zero, SiLU far below zero.  Bars are worst cases of
-the fp32 operations, counted beside each test.
+the others, a mean far from zero, sums over many samples, SiLU far below zero.
+Bars are worst cases of the fp32 operations, counted beside each test.
 """
 import numpy as np
 import pytest
@@ -110,6 +110,29 @@ def test_one_offset_for_all_values(shape, x):
     bar = U + L + (L * mean * rstd) ** 2
     print(f"    1 / std: {(off / bar).max():.3f} of its bar", flush=True)
     assert (off <= bar).all()
+
+
+# ------------------------------------------------ sums over many samples ----
+def test_gradients_of_shift_over_many_samples():
+    """dbeta over 100000 samples of 200 pixels whose gradient is one number a channel:
+    a chain of equal terms rounds the same way at every step, and these numbers are
+    ones for which a chain over 1563 of the samples' sums, exact each,
+    loses more than L of itself.  As bounded in test_gpu_gn.py: 256 operations."""
+    K = _K()
+    n, hw, c = 100000, 200, 8
+    print(f"[gn many samples] {n} x {hw} x {c}", flush=True)
+    v = np.array([56553, 53865, 64279, 33911, 33673, 41719, 57459, 47629]) / 32768
+    g = f32(v).expand(n * hw, c).contiguous()
+    x = torch.zeros(n * hw, c, dtype=torch.bfloat16, device=DEV)
+    d = K.gn_desc(n, hw, c, 1, gtype=K.TYPE_F32)
+    st = torch.cat([torch.zeros(n, device=DEV), torch.ones(n, device=DEV)])
+    dx, dg, db = torch.empty_like(x), torch.empty(c, device=DEV), torch.empty(c, device=DEV)
+    nb = K.op_gn_workspace_bytes(d, True)
+    ws = torch.empty(max(16, nb), dtype=torch.uint8, device=DEV)
+    K.op_gn_backward(d, g, x, st, torch.ones(c, device=DEV), torch.zeros(c, device=DEV), dx, dg, db, ws, nb)
+    err = np.abs(host(db) / (v * (n * hw)) - 1)
+    print(f"    {err.max() / L:.3f} of its bar", flush=True)
+    assert (err <= L).all() and bool((dg == 0).all())
 
 
 # ------------------------------------------------------------------- SiLU --
