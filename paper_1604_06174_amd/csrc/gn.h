@@ -52,6 +52,7 @@ struct GnPlan {
   int NV, teams;
   int pack;  // samples of one pixel that a wavefront takes at once (1: its rows are pixels)
   int64_t rows;
+  int segments;  // their records are added up in so many segments first (1: at once)
   // split: `first` leaves every chunk's sums, `second` applies them, adding them up by
   // itself (`merge`: a launch between them does)
   bool merge;

@@ -308,37 +308,39 @@ __global__ __launch_bounds__(V == 8 ? 512 : 1024) void k_gn_bwd_sums(GnArgs A) {
   channel_record<V, false, RED>(A, tm, 1, tile, by, ch, lds);
 }
 
-// dgamma | dbeta from `rows` records [2][C]: the 16 columns from 16 blk, a thread
-// per column and row in turn, added in a fixed order.  A call of many samples may have
-// a record for each: they are taken eight at a time without conditions (with one per load
-// these waited for each other: the sums of 20000 records of 64 channels 55 us, now 33) and
-// added as a tree.  red: [blockDim / 16][17].
-__device__ __forceinline__ void record_sums(const GnArgs &A, int rows, int blk, float *red) {
+// The sums of `rows` records [2][C] (dgamma | dbeta at the end): the 16 columns from
+// 16 blk, a thread per column and row in turn, added in a fixed order.  A call of many
+// samples may have a record for each: they are taken eight at a time without conditions
+// (with one per load these waited for each other: the backward of 20000 samples of 49
+// pixels x 64 channels took 130 us, without 107) and added as a tree.
+// red: [blockDim / 16][17].
+__device__ __forceinline__ void record_sums(const float *cpart, int rows, int C, int blk, float *out0, float *out1,
+                                            float *red) {
   const int e = blk * 16 + threadIdx.x % 16, r0 = threadIdx.x / 16, R = blockDim.x / 16;
   float s = 0.f;
-  if (e < 2 * A.C) {
-    const float *const part = A.cpart + e;
+  if (e < 2 * C) {
+    const float *const part = cpart + e;
     constexpr int U = 8;
     float v[U];
     int r = r0;
     for (; r + (U - 1) * R < rows; r += U * R) {
 #pragma unroll
-      for (int k = 0; k < U; ++k) v[k] = part[int64_t(r + k * R) * 2 * A.C];
+      for (int k = 0; k < U; ++k) v[k] = part[int64_t(r + k * R) * 2 * C];
       s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
     if (r < rows) {
 #pragma unroll
-      for (int k = 0; k < U; ++k) v[k] = r + k * R < rows ? part[int64_t(r + k * R) * 2 * A.C] : 0.f;
+      for (int k = 0; k < U; ++k) v[k] = r + k * R < rows ? part[int64_t(r + k * R) * 2 * C] : 0.f;
 #pragma unroll
       for (int k = 0; k < U; ++k) s += v[k];
     }
   }
   red[r0 * 17 + threadIdx.x % 16] = s;
   __syncthreads();
-  if (threadIdx.x < 16 && e < 2 * A.C) {
+  if (threadIdx.x < 16 && e < 2 * C) {
     s = 0.f;
     for (int r = 0; r < R; ++r) s += red[r * 17 + threadIdx.x];
-    (e < A.C ? A.dgamma : A.dbeta)[e < A.C ? e : e - A.C] = s;
+    (e < C ? out0 : out1)[e < C ? e : e - C] = s;
   }
 }
 
@@ -349,7 +351,7 @@ __device__ __forceinline__ void record_sums(const GnArgs &A, int rows, int blk, 
 template <typename XT, typename GT_, typename DT, int V, bool MERGED>
 __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, int sums) {
   extern __shared__ float lds[];
-  if (int(blockIdx.x) < sums) return record_sums(A, A.n * A.chunks1, blockIdx.x, lds);
+  if (int(blockIdx.x) < sums) return record_sums(A.cpart, A.n * A.chunks1, A.C, blockIdx.x, A.dgamma, A.dbeta, lds);
   const int t = threadIdx.x, T = blockDim.x, ty = A.by_vc.of(t), tx = t - ty * A.VC;
   const int blk = blockIdx.x - sums, by = A.by_tiles.of(blk), c0 = (blk - by * A.tiles) * A.W, c = c0 + tx * V;
   const int i = A.by_chunks.of(by), p0 = (by - i * A.chunks) * A.chunk, np = min(A.hw - p0, A.chunk);
@@ -473,8 +475,8 @@ __global__ __launch_bounds__(V == 8 ? 256 : 1024) void k_gn_bwd_apply(GnArgs A, 
 
 // many chunks or wide groups: gsum[i][k] = sum a du | sum a du xhat of one group
 void merge_groups(hipStream_t s, const GnArgs &a);
-// dgamma | dbeta from the resident passes' records
-void sum_records(hipStream_t s, const GnArgs &a);
+// dgamma | dbeta from the resident passes' records (gn_plan: in so many segments first)
+void sum_records(hipStream_t s, const GnArgs &a, int segments);
 
 template <typename XT, typename GT_, typename DT, int V, int NV, int NJ>
 void launch_resident(hipStream_t s, const GnPlan &g, const GnArgs &a) {
@@ -517,7 +519,7 @@ void run(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {
       launch_resident<XT, GT_, DT, V, 8, NJ>(s, g, a);
     else if constexpr (V == 1)  // vectors stop at 8 (gn_plan)
       launch_resident<XT, GT_, DT, V, 16, NJ>(s, g, a);
-    if (g.rows > 1) sum_records(s, a);
+    if (g.rows > 1) sum_records(s, a, g.segments);
     return;
   }
   const GnCover &v = g.first, &w = g.second;

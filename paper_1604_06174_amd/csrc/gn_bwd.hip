@@ -50,9 +50,13 @@ __global__ __launch_bounds__(1024) void k_gn_bwd_merge(GnArgs A) {
   }
 }
 
-__global__ __launch_bounds__(1024) void k_gn_records(GnArgs A) {
+// dgamma and dbeta, or (`part`) the record of a segment of `per` of the records
+__global__ __launch_bounds__(1024) void k_gn_records(GnArgs A, int per, float *part) {
   __shared__ float red[64 * 17];
-  record_sums(A, A.rows, blockIdx.x, red);
+  const int r0 = blockIdx.y * per;
+  float *const out = part + int64_t(blockIdx.y) * 2 * A.C;
+  record_sums(A.cpart + int64_t(r0) * 2 * A.C, min(per, A.rows - r0), A.C, blockIdx.x, part ? out : A.dgamma,
+              part ? out + A.C : A.dbeta, red);
 }
 
 }  // namespace
@@ -64,8 +68,17 @@ void merge_groups(hipStream_t s, const GnArgs &a) {
   hipLaunchKernelGGL(k_gn_bwd_merge, dim3(uint32_t(a.n * a.G)), dim3(threads), 0, s, a);
 }
 
-void sum_records(hipStream_t s, const GnArgs &a) {
-  hipLaunchKernelGGL(k_gn_records, dim3((2 * a.C + 15) / 16), dim3(1024), 0, s, a);
+void sum_records(hipStream_t s, const GnArgs &a, int segments) {
+  const uint32_t columns = (2 * a.C + 15) / 16;
+  GnArgs b = a;
+  if (segments > 1) {
+    float *const part = a.cpart + int64_t(a.rows) * 2 * a.C;
+    const int per = (a.rows + segments - 1) / segments;
+    b.rows = (a.rows + per - 1) / per;
+    hipLaunchKernelGGL(k_gn_records, dim3(columns, b.rows), dim3(1024), 0, s, a, per, part);
+    b.cpart = part;
+  }
+  hipLaunchKernelGGL(k_gn_records, dim3(columns), dim3(1024), 0, s, b, b.rows, static_cast<float *>(nullptr));
 }
 
 void run_f32(hipStream_t s, const GnProblem &p, const GnPlan &g, const GnArgs &a) {

@@ -176,7 +176,14 @@ GnPlan gn_plan(const GnProblem &p, bool backward) {
   if (g.resident) {
     v.blocks = g.rows * v.tiles;
     if (!g.wave) reductions(p, backward, backward ? 2 : 1, g);
-    if (backward && g.rows > 1) g.ws_channels = align256(uint64_t(g.rows) * 2 * p.C * 4);
+    if (backward && g.rows > 1) {
+      // 64 threads a column add up the records: more workgroups take part where that is
+      // more than 64 records each (100000 of eight channels, one workgroup: 287 us, 177 in 25
+      // segments; 16384 of 64: 53.6 and 39.7; 8000: 44.6 and 42.1; below, the launch costs what
+      // it gives)
+      g.segments = int(std::min<int64_t>(64, ceil_div(g.rows, 4096)));
+      g.ws_channels = align256(uint64_t(g.rows + (g.segments > 1 ? g.segments : 0)) * 2 * p.C * 4);
+    }
     return g;
   }
   v.threads = int(std::max<int64_t>(256, up(v.VC, 64)));

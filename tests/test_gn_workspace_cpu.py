@@ -25,8 +25,8 @@ def test_rows_of_wide_groups_take_a_few_megabytes(n, c, groups, x):
 
 
 def test_workspace_is_bounded_by_the_tensor_or_a_few_megabytes():
-    """Random sizes: 16 MB, or a record of eight bytes a channel for every sample of five
-    pixels or more (three where the channels are taken one by one)."""
+    """Random sizes: 17 MB, or a record of eight bytes a channel for every sample of five
+    pixels or more (three where the channels are taken one by one), and 64 more."""
     r = random.Random(3)
     for _ in range(20000):
         c = int(2 ** r.uniform(0, 12.5))
@@ -43,4 +43,4 @@ def test_workspace_is_bounded_by_the_tensor_or_a_few_megabytes():
         records = 8 / 5 if c % 8 == 0 and math.lcm(c // groups, 8) <= 4096 else 8 / 3
         for backward in (False, True):
             b = nbytes(n, hw, c, groups, backward, xtype=x)
-            assert b <= max(17 * MB, records * n * hw * c + 4096), (n, hw, c, groups, x, backward, b)
+            assert b <= max(17 * MB, records * n * hw * c + 64 * 8 * c + 4096), (n, hw, c, groups, x, backward, b)
