@@ -350,7 +350,9 @@ __device__ __forceinline__ float gn_exp_neg(float u) {
 }
 
 // FINE: fp32 activations.  bf16 ones take the exponential in two instructions: its
-// relative error, |u| half steps of fp32 below zero, is a ten-thousandth of their own.
+// relative error, 1.25 |u| half steps of fp32, is a thousandth of theirs and less for |u|
+// up to 50.  (fp32 forward of 32 x 3136 pixels x 64 channels 19.8 us, 20.1 FINE; where
+// code has yet to be fetched its 40 bytes an element count: 34 x 102 x 240 9.3 and 10.1.)
 template <bool FINE>
 __device__ __forceinline__ float gn_sigmoid(float u) {
   return __builtin_amdgcn_rcpf(1.f + (FINE ? gn_exp_neg(u) : __expf(-u)));
