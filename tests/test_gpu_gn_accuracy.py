@@ -197,3 +197,27 @@ def test_silu_slope(vec, x):
     err = np.abs(host(db) - want)
     print(f"    {np.max(err / (bar + 1e-37)):.3f} of its bar", flush=True)
     assert (err <= bar + 1e-37).all()
+
+
+@pytest.mark.parametrize("vec", [8, 1])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_silu_of_extremes(vec, x):
+    """Where the exponential under- or overflows: u itself or zero, and slopes of one or
+    zero; NaN and infinity stay what u / (1 + exp(-u)) makes of them."""
+    K = _K()
+    print(f"[gn silu extremes] {vec} {x}", flush=True)
+    big = [200.0, 1e4, 1e30, 2.0 ** 127, 3e38, float("inf")]
+    u = rounded(np.array(big + [-v for v in big[:-1]] + [float("nan"), float("-inf")] + [0.0] * (vec + 2)), x)
+    u = _pad8(u, vec)
+    d, xd, st, ga, be = _identity(u, types()[x][1])
+    y = torch.empty_like(xd)
+    K.op_gn_apply(d, xd, st, ga, be, y)
+    got = host(y.float()).reshape(-1)
+    assert np.array_equal(got[:6], u[:6].astype(np.float64)) and (got[6:11] == 0).all()
+    assert np.isnan(got[11:13]).all() and (got[13:] == 0).all()
+    dx, dg, db = (torch.empty(u.size, device=DEV) for _ in range(3))
+    nb = K.op_gn_workspace_bytes(d, True)
+    ws = torch.empty(max(16, nb), dtype=torch.uint8, device=DEV)
+    K.op_gn_backward(d, torch.full((u.size,), 3.0, device=DEV), xd, st, ga, be, dx, dg, db, ws, nb)
+    got = host(db)
+    assert (got[:5] == 3).all() and (got[6:11] == 0).all() and np.isnan(got[11]) and (got[13:] == 1.5).all()
