@@ -73,7 +73,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_gn_fwd(GnArgs A) {
     group_sums<1, NJ, V, WAVE, RED>(A, tm, s, red);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      cp.mean[j] = s[j] / m;  // not times 1 / m: a constant group's mean is that constant
+      cp.mean[j] = s[j] / m;  // not times 1 / m: exact sums (as of a constant of few bits) give the exact mean
       s[j] = 0.f;
     }
 #pragma unroll
