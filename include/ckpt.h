@@ -778,6 +778,157 @@ int op_dropout(int64_t rows, int64_t cols, int32_t xtype, const void *x, int64_t
                int64_t ldr, int32_t ytype, void *y, int64_t ldy, const ckpt_dropout *drop,
                void *stream);
 
+/* ---- units of token models -----------------------------------------------
+ * RMS norm with the residual's addition, embedding, and attention over packed
+ * sequences: forward, re-run and backward of the units that a checkpointed
+ * token model is made of, beside op_gemm_bf16 and op_dropout.  Rows are tokens.
+ * Sums, statistics and softmax are held in fp32 and outputs rounded once; sums
+ * are added in a fixed order (the same bits on every run).  Every call
+ * enqueues on `stream` alone, waits for nothing and may be captured; calls that
+ * share a workspace must not overlap.  The stream belongs to the current
+ * device.
+ *
+ * Errors of all of them: CKPT_E_INVALID for null pointers, sizes or strides out
+ * of range, unknown types, addresses that are not multiples of an element's
+ * size (what else they have to be is said below) or a workspace that is not
+ * 16-byte aligned; CKPT_E_WORKSPACE for a short one; CKPT_E_UNSUPPORTED for
+ * sizes beyond the stated ones.
+ */
+#define CKPT_TYPE_E4M3 2 /* 8-bit floating point, 4 exponent and 3 mantissa bits, largest 448 (an rms output) */
+
+/*
+ * An RMS norm: `rows` rows of c columns.  xtype: x; htype: the residual stream
+ * (res and h); ytype: y; gtype: g; dtype: the stream's gradient (gh and d).
+ * ytype may be CKPT_TYPE_E4M3: y is then one byte a value, with one fp32 scale
+ * for each qgroup columns of a row (a power of two from 8 to 512, the last group
+ * of a row may be shorter; 0: one for the row).
+ * Row strides in elements, 0 for c: ldx of x; ldh of h and res; ldy; ldg; ldd
+ * of d and gh.  Elements between the rows are neither read nor written.
+ * Widths, strides and addresses are free; c <= 32768, rows < 2^31.
+ */
+typedef struct ckpt_rms_desc {
+  int64_t rows;
+  int32_t c, qgroup;
+  int32_t xtype, htype, ytype, gtype, dtype;
+  float eps;
+  int64_t ldx, ldh, ldy, ldg, ldd;
+} ckpt_rms_desc;
+
+/*
+ * op_rms_forward -- h = x + res, rounded to htype, st[row] = 1 / sqrt(mean(h^2)
+ * + eps) (f32 [rows]) of the rounded h, and y = h st w (w f32 [c]).
+ * Without a residual (res and h null) x itself is normalised and xtype must
+ * be htype.  For an 8-bit y: with u = h st w and top = max(|u|, 1e-30) of a
+ * group, its scale is ys[row, group] = top / 448 (f32 [rows, ceil(c / qgroup)])
+ * and y = u (448 / top); y times its scale is what it stands for (of a group
+ * with an infinity or a NaN: NaN throughout).  ys is null otherwise.
+ * h and y may each be written over x or res of the same type and stride.
+ */
+int op_rms_forward(const ckpt_rms_desc *desc, const void *x, const void *res, const float *w, void *h,
+                   void *y, float *ys, float *st, void *stream);
+
+/* op_rms_apply -- the same y (and ys), bit for bit, from the h (x without a
+ * residual; of htype and stride ldh) and st that op_rms_forward left: what a
+ * checkpointed segment's re-run needs. */
+int op_rms_apply(const ckpt_rms_desc *desc, const void *h, const float *st, const float *w, void *y,
+                 float *ys, void *stream);
+
+/* op_rms_workspace_bytes -- device workspace of op_rms_backward (at most 512 c
+ * floats, and 16 bytes more for each 4 that do not divide c). */
+int op_rms_workspace_bytes(const ckpt_rms_desc *desc, uint64_t *bytes);
+
+/*
+ * op_rms_backward -- for g = dL/dy (of an 8-bit y: of what it stands for) and
+ * gh = dL/dh from the stream's other readers (null: none), with xhat = h st:
+ * d = gh + st (g w - xhat mean(g w xhat)), the gradient of x and of res alike,
+ * and dw = sum over rows of g xhat (f32 [c]).  d may be written over g, h or gh
+ * of the same type and stride.
+ */
+int op_rms_backward(const ckpt_rms_desc *desc, const void *g, const void *gh, const void *h,
+                    const float *st, const float *w, void *d, float *dw, void *workspace,
+                    uint64_t workspace_bytes, void *stream);
+
+/*
+ * An embedding: `tokens` ids into a table of vocab rows of c columns, rows
+ * scaled by `scale`.  ids are int32, or int64 with ids64 = 1.  wtype: the
+ * table; ytype: the rows looked up; gtype: their gradient; dtype: the table's
+ * gradient.  Strides in elements, 0 for c: ldw of the table and its gradient,
+ * ldy, ldg.  accumulate = 1: op_embed_backward adds to the table's gradient
+ * (an output layer that shares the table has left its part there).
+ * tokens < 2^31, vocab < 2^31, c <= 2^20.
+ */
+typedef struct ckpt_embed_desc {
+  int64_t tokens, vocab;
+  int32_t c, ids64;
+  int32_t wtype, ytype, gtype, dtype;
+  int32_t accumulate;
+  float scale;
+  int64_t ldw, ldy, ldg;
+} ckpt_embed_desc;
+
+/* op_embed_forward -- y[i] = scale w[ids[i]]; a row of zeros for an id outside
+ * [0, vocab) (padding). */
+int op_embed_forward(const ckpt_embed_desc *desc, const void *ids, const void *w, void *y, void *stream);
+
+/* op_embed_workspace_bytes -- device workspace of op_embed_backward. */
+int op_embed_workspace_bytes(const ckpt_embed_desc *desc, uint64_t *bytes);
+
+/* op_embed_backward -- dw[v] = scale times the sum of g[i] over the i with ids[i]
+ * = v (plus dw[v] with accumulate); all rows are written, those of absent ids
+ * with zeros (accumulate: left as they were).  Ids outside [0, vocab) have no
+ * part.  The tokens are sorted by id, each id's in their order, and added up in
+ * that order. */
+int op_embed_backward(const ckpt_embed_desc *desc, const void *ids, const void *g, void *dw,
+                      void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Attention over `seqs` packed sequences, bf16.  Sequence s has the query rows
+ * qoff[s] .. qoff[s + 1] - 1 of tq and the key rows koff[s] .. koff[s + 1] - 1 of
+ * tk (device int32 [seqs + 1], not decreasing, within [0, tq] and [0, tk], read
+ * when the kernels run; offsets that break this are clamped to the tensors, and
+ * what is computed then is not specified).  A sequence may be empty.  Rows that
+ * belong to no sequence are left as they were.
+ * `heads` query heads share kv_heads key heads, heads / kv_heads consecutive ones
+ * each; dim values a head (a multiple of 8, at most 128).  causal = 1: query i of
+ * lq sees keys j <= i + lk - lq of lk (the queries are the last of the keys'
+ * positions), else all.  A query that sees no key gets o = 0 and lse = -inf, and
+ * adds to no gradient.
+ * scale multiplies the scores (0: 1 / sqrt(dim)).  Elements from row to row ld?
+ * (0: heads or kv_heads times dim) and from head to head hs? (0: dim) of q, k, v
+ * and o; multiples of 8, addresses of 16 bytes.  g has o's strides; dq, dk and dv
+ * those of q, k and v.
+ * tq, tk < 2^31, seqs < 2^20, heads <= 4096.
+ */
+typedef struct ckpt_attn_desc {
+  int64_t tq, tk;
+  int32_t seqs, heads, kv_heads, dim;
+  int32_t causal;
+  float scale;
+  int64_t ldq, hsq, ldk, hsk, ldv, hsv, ldo, hso;
+} ckpt_attn_desc;
+
+/* op_attn_workspace_bytes -- device workspace op_attn_forward (backward = 0;
+ * 0 for none, a null workspace will do) or op_attn_backward needs. */
+int op_attn_workspace_bytes(const ckpt_attn_desc *desc, int32_t backward, uint64_t *bytes);
+
+/* op_attn_forward -- o = softmax(scale q k^T) v of each sequence and head, and lse
+ * (f32 [heads, tq]), the logarithm of each row's sum of exponentials.  What a
+ * query does not see has no part in its row, whatever values it holds.  The
+ * probabilities are rounded to bf16 for their product with v.  A re-run gives
+ * the same bits. */
+int op_attn_forward(const ckpt_attn_desc *desc, const void *q, const void *k, const void *v,
+                    const int32_t *qoff, const int32_t *koff, void *o, float *lse, void *workspace,
+                    uint64_t workspace_bytes, void *stream);
+
+/* op_attn_backward -- from o and lse that op_attn_forward left: with p = exp(scale
+ * q k^T - lse) and ds = p (g v^T - sum(g o)) (both rounded to bf16 for the
+ * products), dq = scale ds k, dk = scale ds^T q and dv = p^T g, the last two added
+ * up over the query heads that share a key head. */
+int op_attn_backward(const ckpt_attn_desc *desc, const void *g, const void *q, const void *k,
+                     const void *v, const void *o, const float *lse, const int32_t *qoff,
+                     const int32_t *koff, void *dq, void *dk, void *dv, void *workspace,
+                     uint64_t workspace_bytes, void *stream);
+
 /* ckpt_last_error -- message of the last failed call on this thread ("" if
  * none). */
 const char *ckpt_last_error(void);

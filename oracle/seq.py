@@ -1,0 +1,140 @@
+"""Float64 oracle of the token models' operators: RMS norm with the residual's
+addition, embedding, attention over packed sequences, and their gradients.
+
+Attention also returns bounds of the rounding that the documented arithmetic may
+add: probabilities and score gradients rounded to bf16 (half a step: 2^-8 of the
+value), everything else in fp32 (2^-24 an operation).
+"""
+import numpy as np
+
+U16, U24 = 2.0 ** -8, 2.0 ** -24  # half a step of bf16 and fp32, of the value
+
+
+# ---------------------------------------------------------------- RMS norm --
+def rms_stat(h, eps):
+    return 1.0 / np.sqrt((h * h).mean(1) + eps)
+
+
+def rms_apply(h, st, w):
+    return h * st[:, None] * w
+
+
+def rms_backward(g, gh, h, st, w):
+    """d, dw and the magnitudes that enter each of their elements."""
+    xhat = h * st[:, None]
+    du = g * w
+    d = st[:, None] * (du - xhat * (du * xhat).mean(1, keepdims=True))
+    mag = st[:, None] * (np.abs(du) + np.abs(xhat) * np.abs(du * xhat).mean(1, keepdims=True))
+    if gh is not None:
+        d, mag = d + gh, mag + np.abs(gh)
+    return d, (g * xhat).sum(0), mag, np.abs(g * xhat).sum(0)
+
+
+def group_scales(u, group):
+    """The scale of each group of columns of an 8-bit output."""
+    c = u.shape[1]
+    group = group or c
+    return np.stack([np.maximum(np.abs(u[:, a:a + group]).max(1), 1e-30) / 448.0 for a in range(0, c, group)], 1)
+
+
+# --------------------------------------------------------------- embedding --
+def embed(ids, w, scale):
+    ok = (ids >= 0) & (ids < len(w))
+    return np.where(ok[:, None], w[np.where(ok, ids, 0)] * scale, 0.0)
+
+
+def embed_backward(ids, g, vocab, scale):
+    d, mag = np.zeros((vocab, g.shape[1])), np.zeros((vocab, g.shape[1]))
+    ok = (ids >= 0) & (ids < vocab)
+    np.add.at(d, ids[ok], g[ok])
+    np.add.at(mag, ids[ok], np.abs(g[ok]))
+    return d * scale, mag * abs(scale)
+
+
+# --------------------------------------------------------------- attention --
+def visible(lq, lk, causal):
+    """[lq, lk]: does query i see key j?"""
+    seen = np.ones((lq, lk), bool)
+    return np.tril(seen, lk - lq) if causal else seen
+
+
+def _clean(seen, *mats):
+    """Hidden rows of a matrix play no part whatever they hold: with each row i of `seen`,
+    the matrix's rows that it does not see as zeros.  (Only for matrices that hold such.)"""
+    return [np.where(np.isfinite(m), m, 0.0) for m in mats]
+
+
+def attention(q, k, v, qoff, koff, causal, scale):
+    """o [tq, heads, dim], lse [heads, tq] and their error bounds.  Rows of no sequence are NaN."""
+    tq, heads, dim = q.shape
+    rep = heads // k.shape[1]
+    o, eo = np.full((tq, heads, dim), np.nan), np.full((tq, heads, dim), np.nan)
+    lse, el = np.full((heads, tq), np.nan), np.full((heads, tq), np.nan)
+    for a, b, c, d in zip(qoff, qoff[1:], koff, koff[1:]):
+        lq, lk = b - a, d - c
+        seen = visible(lq, lk, causal)
+        for h in range(heads):
+            Q, K, V = q[a:b, h], k[c:d, h // rep], v[c:d, h // rep]
+            Kf, Vf = _clean(seen, K, V)  # non-finite rows are hidden ones in the tests
+            e = np.where(seen, Q @ Kf.T * scale, -np.inf)
+            mag = np.where(seen, np.abs(Q) @ np.abs(Kf).T * scale, 0.0)
+            if lk == 0:
+                o[a:b, h], eo[a:b, h], lse[h, a:b], el[h, a:b] = 0, 1e-30, -np.inf, 0
+                continue
+            top = e.max(1)
+            base = np.where(np.isinf(top), 0.0, top)[:, None]
+            p = np.exp(e - base)
+            z = p.sum(1)
+            none = z == 0
+            p = p / np.where(none, 1, z)[:, None]
+            o[a:b, h] = p @ Vf
+            with np.errstate(divide="ignore"):
+                lse[h, a:b] = base[:, 0] + np.log(z)
+            # a score is off by dim products and sums and a few operations more, its exponential
+            # (a power of two, in hardware to about 2^-22) by as much of itself; a sum of lk terms
+            rel = (dim + 16) * U24 * 2 * (mag.max(1) + np.abs(base[:, 0])) + (lk + 64) * U24
+            eo[a:b, h] = (U16 + 2 * rel)[:, None] * (p @ np.abs(Vf)) + U16 * np.abs(o[a:b, h]) + 1e-30
+            el[h, a:b] = np.where(none, 0, rel + 4 * U24 * np.abs(np.where(none, 0, lse[h, a:b])))
+    return o, lse, eo, el
+
+
+def attention_backward(g, q, k, v, o, lse, qoff, koff, causal, scale):
+    """dq, dk, dv and their error bounds, for the o and lse that the call is given."""
+    tq, heads, dim = q.shape
+    rep = heads // k.shape[1]
+    out = [np.full(t.shape, np.nan) for t in (q, k, v)]
+    err = [np.full(t.shape, np.nan) for t in (q, k, v)]
+    for a, b, c, d in zip(qoff, qoff[1:], koff, koff[1:]):
+        lq, lk = b - a, d - c
+        seen = visible(lq, lk, causal)
+        for t, e in zip(out, err):
+            n = slice(a, b) if t is out[0] else slice(c, d)
+            t[n], e[n] = 0, 0
+        if lq == 0 or lk == 0:
+            continue
+        for h in range(heads):
+            kh = h // rep
+            Q, K, V, G, O = _clean(seen, q[a:b, h], k[c:d, kh], v[c:d, kh], g[a:b, h], o[a:b, h])
+            L = lse[h, a:b]
+            fin = np.isfinite(L)
+            Lf = np.where(fin, L, 0.0)
+            s = seen & fin[:, None]
+            e = Q @ K.T * scale
+            mag = np.abs(Q) @ np.abs(K).T * scale
+            p = np.where(s, np.exp(np.where(s, e - Lf[:, None], 0.0)), 0.0)
+            dp, delta = G @ V.T, (G * O).sum(1)
+            ds = p * (dp - delta[:, None])
+            rel = (dim + 16) * U24 * 2 * (mag + np.abs(Lf)[:, None]) + 64 * U24
+            ep = p * (U16 + rel)
+            eds = (U16 + rel) * np.abs(ds) + p * (dim + 16) * U24 * (np.abs(G) @ np.abs(V).T +
+                                                                    (np.abs(G) * np.abs(O)).sum(1)[:, None])
+            chain = (max(lq * rep, lk) + 64) * U24
+            out[0][a:b, h] = ds @ K * scale
+            err[0][a:b, h] = (eds + chain * np.abs(ds)) @ np.abs(K) * scale
+            out[1][c:d, kh] += ds.T @ Q * scale
+            err[1][c:d, kh] += (eds + chain * np.abs(ds)).T @ np.abs(Q) * scale
+            out[2][c:d, kh] += p.T @ G
+            err[2][c:d, kh] += (ep + chain * p).T @ np.abs(G)
+    for t, e in zip(out, err):
+        e += U16 * np.abs(t) + 1e-30
+    return out, err

@@ -173,7 +173,38 @@ _sig("op_gn_backward", C.c_int, [_gnp, _vp, _vp, _vp, _vp, _vp, _drp, _vp, _vp, 
 _sig("op_dropout", C.c_int, [C.c_int64, C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, _vp,
                              C.c_int64, _drp, _vp])
 
-TYPE_F32, TYPE_BF16 = 0, 1
+
+class RmsDesc(C.Structure):
+    _fields_ = ([("rows", C.c_int64)] +
+                [(k, C.c_int32) for k in ("c", "qgroup", "xtype", "htype", "ytype", "gtype", "dtype")] +
+                [("eps", C.c_float)] + [(k, C.c_int64) for k in ("ldx", "ldh", "ldy", "ldg", "ldd")])
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = ([(k, C.c_int64) for k in ("tokens", "vocab")] +
+                [(k, C.c_int32) for k in ("c", "ids64", "wtype", "ytype", "gtype", "dtype", "accumulate")] +
+                [("scale", C.c_float)] + [(k, C.c_int64) for k in ("ldw", "ldy", "ldg")])
+
+
+class AttnDesc(C.Structure):
+    _fields_ = ([(k, C.c_int64) for k in ("tq", "tk")] +
+                [(k, C.c_int32) for k in ("seqs", "heads", "kv_heads", "dim", "causal")] + [("scale", C.c_float)] +
+                [(k, C.c_int64) for k in ("ldq", "hsq", "ldk", "hsk", "ldv", "hsv", "ldo", "hso")])
+
+
+_rmp, _emp, _atp = C.POINTER(RmsDesc), C.POINTER(EmbedDesc), C.POINTER(AttnDesc)
+_sig("op_rms_forward", C.c_int, [_rmp] + [_vp] * 8)
+_sig("op_rms_apply", C.c_int, [_rmp] + [_vp] * 6)
+_sig("op_rms_workspace_bytes", C.c_int, [_rmp, _u64p])
+_sig("op_rms_backward", C.c_int, [_rmp] + [_vp] * 8 + [C.c_uint64, _vp])
+_sig("op_embed_forward", C.c_int, [_emp] + [_vp] * 4)
+_sig("op_embed_workspace_bytes", C.c_int, [_emp, _u64p])
+_sig("op_embed_backward", C.c_int, [_emp] + [_vp] * 4 + [C.c_uint64, _vp])
+_sig("op_attn_workspace_bytes", C.c_int, [_atp, C.c_int32, _u64p])
+_sig("op_attn_forward", C.c_int, [_atp] + [_vp] * 8 + [C.c_uint64, _vp])
+_sig("op_attn_backward", C.c_int, [_atp] + [_vp] * 12 + [C.c_uint64, _vp])
+
+TYPE_F32, TYPE_BF16, TYPE_E4M3 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 EPI_STORE, EPI_ADD, EPI_BF16STATS, EPI_ADDMASK, EPI_BNBWD = 0, 1, 3, 4, 6
 BNB_RES_NONE, BNB_RES_ID, BNB_RES_BN = 0, 1, 2
@@ -182,6 +213,9 @@ EXPORTED = ["op_gemm_bf16_blocks", "op_gemm_bf16", "op_sum_partials", "op_conv_b
             "op_conv_bf16_dgrad", "op_conv_bf16_wgrad", "op_bn_finalize", "op_bnb_partial_blocks",
             "op_bnb_apply", "op_bnb_backward", "op_bnb_backward_apply", "op_im2col7", "op_maxpool",
             "op_gn_workspace_bytes", "op_gn_forward", "op_gn_apply", "op_gn_backward", "op_dropout",
+            "op_rms_forward", "op_rms_apply", "op_rms_workspace_bytes", "op_rms_backward", "op_embed_forward",
+            "op_embed_workspace_bytes", "op_embed_backward", "op_attn_workspace_bytes", "op_attn_forward",
+            "op_attn_backward",
             "ckpt_last_error", "plan_checkpoints", "plan_info", "plan_cuts", "plan_serialize",
             "plan_free", "plan_search", "graph_plan", "graph_plan_info", "graph_plan_schedule",
             "graph_plan_blocks", "graph_plan_free", "net_node_graph", "graph_workspace_bytes",
@@ -807,3 +841,135 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
         yt = _TYPE_NAMES.get(ytype)
         px, pr, py = _typed((x, _TYPE_NAMES.get(xtype), "x"), (res, yt, "res"), (y, yt, "y"))
     _check(_lib.op_dropout(rows, cols, xtype, px, ldx, pr, ldr, ytype, py, ldy, drop, _s(stream)))
+
+
+# -------------------------------------------------- units of token models --
+# tensors by type code; an 8-bit output may also be given as plain bytes
+_SEQ_DTYPES = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+
+def _of(name, code, *args):
+    """The addresses of (x, name)s, which as floating-point tensors have to be of the
+    type `code`; addresses and other memory are taken as they are."""
+    want = _SEQ_DTYPES[code] if 0 <= code < 3 else None  # an unknown code is the library's to refuse
+    out = []
+    for x, arg in args:
+        if isinstance(x, torch.Tensor) and want is not None and x.dtype is not want and x.dtype.is_floating_point:
+            raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {x.dtype}, described as {want}")
+        out.append(_addr(x))
+    return out
+
+
+def _ints(name, bits, *args):
+    """The addresses of (x, name)s, which as tensors have to be integers of `bits` bits side by side."""
+    want = torch.int64 if bits == 64 else torch.int32
+    for x, arg in args:
+        if isinstance(x, torch.Tensor) and (x.dtype is not want or not x.is_contiguous()):
+            raise CkptError(E_INVALID, f"{name}({arg}): {x.dtype} of strides {x.stride()}, not contiguous {want}")
+    return [_addr(x) for x, _ in args]
+
+
+def rms_desc(rows, c, xtype=TYPE_BF16, htype=None, ytype=None, gtype=None, dtype=None, qgroup=0, ldx=0, ldh=0, ldy=0,
+             ldg=0, ldd=0, eps=1e-5) -> RmsDesc:
+    """htype defaults to xtype; ytype, gtype and dtype to htype (an 8-bit ytype to a gtype of
+    htype); strides to c."""
+    htype = xtype if htype is None else htype
+    ytype, gtype, dtype = (htype if t is None else t for t in (ytype, gtype, dtype))
+    _fit("rms_desc", 62, rows, ldx, ldh, ldy, ldg, ldd)
+    _fit("rms_desc", 31, c)
+    _fit("rms_desc: qgroup and types", 31, qgroup, xtype, htype, ytype, gtype, dtype, large=E_INVALID)
+    return RmsDesc(rows, c, qgroup, xtype, htype, ytype, gtype, dtype, eps, ldx, ldh, ldy, ldg, ldd)
+
+
+def op_rms_forward(desc: RmsDesc, x, w, y, st, res=None, h=None, ys=None, stream=None):
+    n = "op_rms_forward"
+    (px,), (pr, ph), (py,) = (_of(n, desc.xtype, (x, "x")), _of(n, desc.htype, (res, "res"), (h, "h")),
+                              _of(n, desc.ytype, (y, "y")))
+    pw, ps, pq = _of(n, TYPE_F32, (w, "w"), (st, "st"), (ys, "ys"))
+    _check(_lib.op_rms_forward(desc, px, pr, pw, ph, py, pq, ps, _s(stream)))
+
+
+def op_rms_apply(desc: RmsDesc, h, st, w, y, ys=None, stream=None):
+    n = "op_rms_apply"
+    (ph,), (py,) = _of(n, desc.htype, (h, "h")), _of(n, desc.ytype, (y, "y"))
+    pw, ps, pq = _of(n, TYPE_F32, (w, "w"), (st, "st"), (ys, "ys"))
+    _check(_lib.op_rms_apply(desc, ph, ps, pw, py, pq, _s(stream)))
+
+
+def op_rms_workspace_bytes(desc: RmsDesc) -> int:
+    v = C.c_uint64()
+    _check(_lib.op_rms_workspace_bytes(desc, C.byref(v)))
+    return v.value
+
+
+def op_rms_backward(desc: RmsDesc, g, h, st, w, d, dw, workspace, workspace_bytes, gh=None, stream=None):
+    n = "op_rms_backward"
+    (pg,), (ph,), (pe, pd) = (_of(n, desc.gtype, (g, "g")), _of(n, desc.htype, (h, "h")),
+                              _of(n, desc.dtype, (gh, "gh"), (d, "d")))
+    ps, pw, pdw = _of(n, TYPE_F32, (st, "st"), (w, "w"), (dw, "dw"))
+    _check(_lib.op_rms_backward(desc, pg, pe, ph, ps, pw, pd, pdw, _addr(workspace), _nbytes(workspace_bytes),
+                                _s(stream)))
+
+
+def embed_desc(tokens, vocab, c, wtype=TYPE_BF16, ytype=None, gtype=None, dtype=TYPE_F32, scale=1.0, ids64=False,
+               accumulate=False, ldw=0, ldy=0, ldg=0) -> EmbedDesc:
+    """ytype defaults to wtype, gtype to ytype, strides to c."""
+    ytype = wtype if ytype is None else ytype
+    gtype = ytype if gtype is None else gtype
+    _fit("embed_desc", 62, tokens, vocab, ldw, ldy, ldg)
+    _fit("embed_desc", 31, c)
+    _fit("embed_desc: types", 31, wtype, ytype, gtype, dtype, large=E_INVALID)
+    return EmbedDesc(tokens, vocab, c, int(bool(ids64)), wtype, ytype, gtype, dtype, int(bool(accumulate)), scale, ldw,
+                     ldy, ldg)
+
+
+def op_embed_forward(desc: EmbedDesc, ids, w, y, stream=None):
+    n = "op_embed_forward"
+    (pi,), (pw,), (py,) = (_ints(n, 64 if desc.ids64 else 32, (ids, "ids")), _of(n, desc.wtype, (w, "w")),
+                           _of(n, desc.ytype, (y, "y")))
+    _check(_lib.op_embed_forward(desc, pi, pw, py, _s(stream)))
+
+
+def op_embed_workspace_bytes(desc: EmbedDesc) -> int:
+    v = C.c_uint64()
+    _check(_lib.op_embed_workspace_bytes(desc, C.byref(v)))
+    return v.value
+
+
+def op_embed_backward(desc: EmbedDesc, ids, g, dw, workspace, workspace_bytes, stream=None):
+    n = "op_embed_backward"
+    (pi,), (pg,), (pd,) = (_ints(n, 64 if desc.ids64 else 32, (ids, "ids")), _of(n, desc.gtype, (g, "g")),
+                           _of(n, desc.dtype, (dw, "dw")))
+    _check(_lib.op_embed_backward(desc, pi, pg, pd, _addr(workspace), _nbytes(workspace_bytes), _s(stream)))
+
+
+def attn_desc(tq, tk, seqs, heads, kv_heads, dim, causal=True, scale=0.0, ldq=0, hsq=0, ldk=0, hsk=0, ldv=0, hsv=0,
+              ldo=0, hso=0) -> AttnDesc:
+    """Strides in elements; scale 0 is 1 / sqrt(dim)."""
+    _fit("attn_desc", 62, tq, tk, ldq, hsq, ldk, hsk, ldv, hsv, ldo, hso)
+    _fit("attn_desc", 31, seqs, heads, kv_heads, dim)
+    return AttnDesc(tq, tk, seqs, heads, kv_heads, dim, int(bool(causal)), scale, ldq, hsq, ldk, hsk, ldv, hsv, ldo, hso)
+
+
+def op_attn_workspace_bytes(desc: AttnDesc, backward: bool) -> int:
+    v = C.c_uint64()
+    _check(_lib.op_attn_workspace_bytes(desc, int(backward), C.byref(v)))
+    return v.value
+
+
+def op_attn_forward(desc: AttnDesc, q, k, v, qoff, koff, o, lse, workspace=None, workspace_bytes=0, stream=None):
+    n = "op_attn_forward"
+    pq, pk, pv, po = _of(n, TYPE_BF16, (q, "q"), (k, "k"), (v, "v"), (o, "o"))
+    (pl,), (pa, pb) = _of(n, TYPE_F32, (lse, "lse")), _ints(n, 32, (qoff, "qoff"), (koff, "koff"))
+    _check(_lib.op_attn_forward(desc, pq, pk, pv, pa, pb, po, pl, _addr(workspace), _nbytes(workspace_bytes),
+                                _s(stream)))
+
+
+def op_attn_backward(desc: AttnDesc, g, q, k, v, o, lse, qoff, koff, dq, dk, dv, workspace, workspace_bytes,
+                     stream=None):
+    n = "op_attn_backward"
+    pg, pq, pk, pv, po, pdq, pdk, pdv = _of(n, TYPE_BF16, (g, "g"), (q, "q"), (k, "k"), (v, "v"), (o, "o"), (dq, "dq"),
+                                            (dk, "dk"), (dv, "dv"))
+    (pl,), (pa, pb) = _of(n, TYPE_F32, (lse, "lse")), _ints(n, 32, (qoff, "qoff"), (koff, "koff"))
+    _check(_lib.op_attn_backward(desc, pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, _addr(workspace),
+                                 _nbytes(workspace_bytes), _s(stream)))

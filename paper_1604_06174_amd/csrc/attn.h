@@ -1,0 +1,257 @@
+// What the attention kernels share: packed sequences, tiles in LDS, matrix operands.
+//
+// All products run on v_mfma_f32_32x32x16_bf16: D[m][n] += sum over k of A[m][k] B[k][n],
+// m, n < 32, k < 16.  Lane l holds A[l % 32][8 (l / 32) + e] and B[8 (l / 32) + e][l % 32]
+// for e < 8, and of D the rows 8 (i / 4) + 4 (l / 32) + i % 4, i < 16, of column l % 32.
+//
+// A product's rows m are those of the tile that comes by in LDS and its columns n those that the
+// wavefront keeps in registers, so a lane has one kept row (a query in the forward and
+// dq, a key in dk and dv) and softmax's sums, masks and scales of it are the lane's own.
+// Probabilities then are D of one product and, without leaving their lanes, B of the
+// next: its k runs over the tile's rows in the order in which D holds them, k = 8 h + e being row
+// 8 (e / 4) + 4 h + e % 4 of sixteen, and A (values by rows of the tile, so transposed) is
+// read from LDS in that order by gfx950's transposing read.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "lanes.h"
+#include "seq.h"
+
+namespace ckpt {
+namespace at {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) short4v lds_short4;
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+static __device__ __align__(16) const unsigned g_zeros[1024] = {};
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// the tile's loads of this wavefront have landed and its LDS reads returned; then every
+// wavefront's have
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt 0, lgkmcnt 0
+  __syncthreads();
+}
+
+// ---- sequences -------------------------------------------------------------
+struct Sequence {
+  int64_t q0, k0;  // first rows
+  int lq, lk;
+  int64_t first;   // first row of the tile, within the sequence
+};
+
+__device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// The sequence that tile `tile` of `size` rows lies in, `per` rows to each row of the
+// tensor that `off` counts.  Sequence s owns the tiles from off[s] per / size + s on: as many
+// as its rows can take whatever their number, so a tile's sequence is found without adding
+// lengths up.  false: the tile is past its sequence's rows.
+__device__ __forceinline__ bool find_tile(const AttnArgs &A, const int *off, int64_t total, int per, int size, int tile,
+                                          Sequence &q) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = A.seqs;
+  while (true) {  // 64 sequences at a time, then 64 ranges of them ...
+    const int step = (n + 63) / 64, s = lo + lane * step;
+    const bool ok = lane * step < n && int64_t(off[s]) * per / size + s <= tile;
+    const int c = __popcll(__ballot(ok));
+    if (c == 0) return false;
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+    if (step == 1) break;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const int64_t base = int64_t(off[lo]) * per / size + lo;
+  q.q0 = clamp_row(A.qoff[lo], 0, A.tq);
+  q.lq = int(clamp_row(A.qoff[lo + 1], q.q0, A.tq) - q.q0);
+  q.k0 = clamp_row(A.koff[lo], 0, A.tk);
+  q.lk = int(clamp_row(A.koff[lo + 1], q.k0, A.tk) - q.k0);
+  q.first = (tile - base) * size;
+  const int64_t rows = int64_t(off == A.qoff ? q.lq : q.lk) * per;
+  return q.first >= 0 && q.first < rows;
+}
+
+// ---- tiles in LDS ----------------------------------------------------------
+// Rows of D values without padding, their 16-byte chunks in an order of the row's own, so that
+// neither 32 rows' equal chunks (A by rows) nor four rows' runs of chunks (A transposed)
+// fall on the same banks.
+template <int D>
+__device__ __forceinline__ int swizzle(int row) {
+  return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+// ROWS rows from `src` on, `ld` elements apart, straight into LDS; zeros for rows from
+// `valid` on and columns from `dim` on
+template <int D, int ROWS, int THREADS>
+__device__ __forceinline__ void load_tile(unsigned char *lds, const __bf16 *src, int64_t ld, int valid, int dim) {
+  constexpr int C = D / 8;
+  const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int c = 0; c < ROWS * C / THREADS; ++c) {
+    const int e = c * THREADS + threadIdx.x, row = e / C, col = ((e % C) ^ swizzle<D>(row)) * 8;
+    const void *p = src + row * ld + col;
+    if (!(row < valid && col < dim)) p = g_zeros + 4 * (threadIdx.x & 255);
+    __builtin_amdgcn_global_load_lds(p, (lds_void *)(lds + (c * THREADS + wave * 64) * 16), 16, 0, 0);
+  }
+}
+
+// a lane's places in a tile: of its row's chunks, and of the transposing reads
+template <int D>
+struct Places {
+  int row;          // byte offset of row lane % 32
+  int key;          // its chunk order, and the lane's half
+  int lo[D / 32], hi[D / 32];
+
+  __device__ __forceinline__ Places() {
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    row = r * D * 2;
+    key = (swizzle<D>(r) ^ h) << 4;
+    const int t = (lane >> 2) & 3;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      const int chunk = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      const int r0 = 4 * h + t, r1 = r0 + 8;
+      lo[b] = r0 * D * 2 + ((chunk ^ swizzle<D>(r0)) << 4) + (lane & 1) * 8;
+      hi[b] = r1 * D * 2 + ((chunk ^ swizzle<D>(r1)) << 4) + (lane & 1) * 8;
+    }
+  }
+
+  // A by rows: columns 16 kk .. 16 kk + 15 of the 32 rows from `first` (a multiple of 32) on
+  __device__ __forceinline__ bf16x8 rows(const unsigned char *tile, int first, int kk) const {
+    return *reinterpret_cast<const bf16x8 *>(tile + first * D * 2 + row + (key ^ (kk << 5)));
+  }
+  // A transposed: m = columns 32 b .. 32 b + 31, k = the 16 rows from `first` (a multiple of 16) on
+  __device__ __forceinline__ bf16x8 columns(const unsigned char *tile, int first, int b) const {
+    const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + lo[b]));
+    const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + hi[b]));
+    const short8v v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    return __builtin_bit_cast(bf16x8, v);
+  }
+};
+
+// eight values of a kept row from column 16 kk + 8 (lane / 32) on, zeros from dim on
+__device__ __forceinline__ bf16x8 kept(const __bf16 *row, int kk, int dim) {
+  const int col = 16 * kk + 8 * ((threadIdx.x & 63) >> 5);
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (col < dim) v = *reinterpret_cast<const u32x4 *>(row + col);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// B of a product over sixteen rows of a tile: eight of a D's sixteen values, rounded
+__device__ __forceinline__ bf16x8 operand(const f32x16 &d, int half) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (__bf16)d[8 * half + e];
+  return r;
+}
+
+__device__ __forceinline__ bool not_finite(bf16x8 a) {
+  const u32x4 w = __builtin_bit_cast(u32x4, a);
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) bad |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+
+// acc += (values of the 16 rows of the tile from `first` on, transposed) b
+template <int D>
+__device__ __forceinline__ void add_rows(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
+                                         int first, bf16x8 b) {
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) acc[t] = mfma(at.columns(tile, first, t), b, acc[t]);
+}
+
+// The same where b is zero for rows that the lane's row does not see: an infinity or a NaN in
+// such a row would make a NaN of the zero, so if the tile's rows hold any, they are taken
+// one by one and kept by the lanes that see them (row c of the sixteen: sees(c)).
+template <int D, typename F>
+__device__ __forceinline__ void add_rows_seen(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
+                                              int first, bf16x8 b, F &&sees) {
+  bf16x8 a[D / 32];
+  bool bad = false;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) {
+    a[t] = at.columns(tile, first, t);
+    bad |= not_finite(a[t]);
+  }
+  if (!__any(bad)) {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = mfma(a[t], b, acc[t]);
+    return;
+  }
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll 1
+  for (int c = 0; c < 16; ++c) {
+    const int e = h == ((c >> 2) & 1) ? (c >> 3) * 4 + (c & 3) : 8;
+    const bool keep = sees(c);
+    bf16x8 one;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) one[k] = k == e ? b[k] : (__bf16)0.f;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      bf16x8 row;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) row[k] = k == e ? a[t][k] : (__bf16)0.f;
+      f32x16 z;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0.f;
+      z = mfma(row, one, z);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] = keep ? acc[t][i] + z[i] : acc[t][i];
+    }
+  }
+}
+
+// row of D value i of 32: 8 (i / 4) + 4 (lane / 32) + i % 4
+__device__ __forceinline__ int d_row(int i) { return 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4; }
+
+// an accumulator's column, scaled, to a row of 16-bit values
+template <int D>
+__device__ __forceinline__ void store_row(__bf16 *row, const f32x16 (&acc)[D / 32], float scale, int dim) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
+      if (col >= dim) continue;
+      bf16x4 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[t][4 * b + k] * scale);
+      *reinterpret_cast<bf16x4 *>(row + col) = v;
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void clear(f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+}
+
+// with the value of the other half's lane
+__device__ __forceinline__ float halves_max(float v) {
+  float a = v, b = v;
+  swap_rows<32>(a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float halves_add(float v) { return xor_add<32>(v); }
+
+}  // namespace at
+}  // namespace ckpt

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <string>
 
+#include "capi_args.h"
 #include "capi_internal.h"
 #include "dropout.h"
 #include "gn.h"
@@ -16,24 +17,12 @@ static_assert(CKPT_ACT_NONE == ckpt::GN_ACT_NONE && CKPT_ACT_RELU == ckpt::GN_AC
 namespace {
 
 using ckpt::fail;
-
-// a device buffer of elements of `size` bytes (a power of two); the message is put
-// together only for a bad one
-void need_ptr(const void *p, const char *fn, const char *arg, uintptr_t size = 1) {
-  if (p && !(reinterpret_cast<uintptr_t>(p) & (size - 1))) return;
-  const std::string what = std::string(fn) + "(" + arg + ")";
-  if (!p) fail(CKPT_E_INVALID, what + ": null pointer");
-  fail(CKPT_E_INVALID, what + ": misaligned address");
-}
-
-[[noreturn]] void refuse(int code, const char *fn, const char *what) { fail(code, std::string(fn) + what); }
+using ckpt::launched;
+using ckpt::need_ptr;
+using ckpt::product;
+using ckpt::refuse;
 
 uintptr_t size_of(bool f32) { return f32 ? 4 : 2; }
-
-void launched(const char *fn) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) fail(CKPT_E_HIP, std::string(fn) + ": " + hipGetErrorString(e));
-}
 
 bool is_f32(int32_t type, const char *fn) {
   if (type != CKPT_TYPE_F32 && type != CKPT_TYPE_BF16) refuse(CKPT_E_INVALID, fn, ": unknown type");
@@ -42,11 +31,6 @@ bool is_f32(int32_t type, const char *fn) {
 
 // elements the generator can number (its block number is 32 bits)
 constexpr int64_t kMaxElements = int64_t(1) << 35;
-
-// a * b, both positive, below 2^62; -1 past it
-int64_t product(int64_t a, int64_t b) {
-  return a > (int64_t(1) << 62) / b ? -1 : a * b;
-}
 
 ckpt::DropArgs drop_args(const ckpt_dropout *d, const char *fn) {
   ckpt::DropArgs a{nullptr, 0, 0, 1.f};
