@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "lanes.h"
 #include "seq.h"
@@ -95,32 +96,44 @@ __device__ __forceinline__ int swizzle(int row) {
   return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-// ROWS rows from `src` on, `ld` elements apart, straight into LDS; zeros for rows from
-// `valid` on and columns from `dim` on
+// The loader of a tile of ROWS rows, `ld` elements apart, straight into LDS: zeros for rows
+// from `valid` on and columns from `dim` on.  A thread loads the same columns of each of its
+// rows, whose order of chunks is the same (they are sixteen rows apart, or 32).
 template <int D, int ROWS, int THREADS>
-__device__ __forceinline__ void load_tile(unsigned char *lds, const __bf16 *src, int64_t ld, int valid, int dim) {
-  constexpr int C = D / 8;
-  const int wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int c = 0; c < ROWS * C / THREADS; ++c) {
-    const int e = c * THREADS + threadIdx.x, row = e / C, col = ((e % C) ^ swizzle<D>(row)) * 8;
-    const void *p = src + row * ld + col;
-    if (!(row < valid && col < dim)) p = g_zeros + 4 * (threadIdx.x & 255);
-    __builtin_amdgcn_global_load_lds(p, (lds_void *)(lds + (c * THREADS + wave * 64) * 16), 16, 0, 0);
+struct Loader {
+  static constexpr int C = D / 8, STEP = THREADS / C, N = ROWS / STEP;
+  static_assert(STEP % 16 == 0 && ROWS % STEP == 0, "rows with the same order of chunks");
+  const __bf16 *src;  // the thread's first chunk of row 0's tile
+  int64_t ld;
+  bool in;            // its columns are below dim
+
+  __device__ __forceinline__ Loader(const __bf16 *base, int64_t ld_, int dim) : ld(ld_) {
+    const int row = threadIdx.x / C, col = ((threadIdx.x % C) ^ swizzle<D>(row)) * 8;
+    src = base + row * ld + col;
+    in = col < dim;
   }
-}
+  // the tile from row `first` on, `offset` elements further
+  __device__ __forceinline__ void load(unsigned char *lds, int64_t first, int valid, int64_t offset = 0) const {
+    const __bf16 *p = src + first * ld + offset;
+    unsigned char *const to = lds + (threadIdx.x >> 6) * 1024;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const bool ok = in && int(threadIdx.x / C) + c * STEP < valid;
+      const void *const q = ok ? static_cast<const void *>(p + c * STEP * ld) : g_zeros + 4 * (threadIdx.x & 255);
+      __builtin_amdgcn_global_load_lds(q, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
+    }
+  }
+};
 
 // a lane's places in a tile: of its row's chunks, and of the transposing reads
 template <int D>
 struct Places {
-  int row;          // byte offset of row lane % 32
-  int key;          // its chunk order, and the lane's half
+  int row;  // byte offset of chunk lane / 32 of row lane % 32; chunk 2 kk further on: ^ kk << 5
   int lo[D / 32], hi[D / 32];
 
   __device__ __forceinline__ Places() {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-    row = r * D * 2;
-    key = (swizzle<D>(r) ^ h) << 4;
+    row = r * D * 2 + ((swizzle<D>(r) ^ h) << 4);
     const int t = (lane >> 2) & 3;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
@@ -130,10 +143,20 @@ struct Places {
       hi[b] = r1 * D * 2 + ((chunk ^ swizzle<D>(r1)) << 4) + (lane & 1) * 8;
     }
   }
+  // A copy that the compiler takes for new values.  A tile's address in LDS is then an offset
+  // within the reads; otherwise its sum with every place is formed before the loop, and
+  // four tiles' sums take the registers of an accumulator.
+  __device__ __forceinline__ Places here() const {
+    Places p = *this;
+    asm volatile("" : "+v"(p.row));
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) asm volatile("" : "+v"(p.lo[b]), "+v"(p.hi[b]));
+    return p;
+  }
 
   // A by rows: columns 16 kk .. 16 kk + 15 of the 32 rows from `first` (a multiple of 32) on
   __device__ __forceinline__ bf16x8 rows(const unsigned char *tile, int first, int kk) const {
-    return *reinterpret_cast<const bf16x8 *>(tile + first * D * 2 + row + (key ^ (kk << 5)));
+    return *reinterpret_cast<const bf16x8 *>(tile + first * D * 2 + (row ^ (kk << 5)));
   }
   // A transposed: m = columns 32 b .. 32 b + 31, k = the 16 rows from `first` (a multiple of 16) on
   __device__ __forceinline__ bf16x8 columns(const unsigned char *tile, int first, int b) const {
@@ -160,12 +183,36 @@ __device__ __forceinline__ bf16x8 operand(const f32x16 &d, int half) {
   return r;
 }
 
-__device__ __forceinline__ bool not_finite(bf16x8 a) {
-  const u32x4 w = __builtin_bit_cast(u32x4, a);
-  bool bad = false;
+// use(i, load(i)) for i < N, each load AHEAD uses before its own and none earlier: left to itself
+// the compiler starts all of them first, and the registers they land in push accumulators
+// out to memory
+template <int N, int AHEAD, typename L, typename U>
+__device__ __forceinline__ void in_turn(L &&load, U &&use) {
+  decltype(load(0)) f[N];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) bad |= (w[k] & 0x7f80u) == 0x7f80u || (w[k] & 0x7f800000u) == 0x7f800000u;
-  return bad;
+  for (int i = 0; i < AHEAD && i < N; ++i) f[i] = load(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i + AHEAD < N) f[i + AHEAD] = load(i + AHEAD);
+    use(i, f[i]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// magnitudes above the largest finite one as that one (as pairs of 16 bits without the sign,
+// infinities and NaNs are the larger numbers); `bad` is not 0 if there were any
+__device__ __forceinline__ bf16x8 finite(bf16x8 a, unsigned &bad) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const u16x2 most = {0x7f7f, 0x7f7f};
+  u32x4 w = __builtin_bit_cast(u32x4, a);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const u16x2 m = __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu);
+    const unsigned f = __builtin_bit_cast(unsigned, __builtin_elementwise_min(m, most)) | (w[k] & 0x80008000u);
+    bad |= f ^ w[k];
+    w[k] = f;
+  }
+  return __builtin_bit_cast(bf16x8, w);
 }
 
 // acc += (values of the 16 rows of the tile from `first` on, transposed) b
@@ -177,48 +224,66 @@ __device__ __forceinline__ void add_rows(f32x16 (&acc)[D / 32], const Places<D> 
 }
 
 // The same where b is zero for rows that the lane's row does not see: an infinity or a NaN in
-// such a row would make a NaN of the zero, so if the tile's rows hold any, they are taken
-// one by one and kept by the lanes that see them (row c of the sixteen: sees(c)).
+// such a row would make a NaN of the zero, so only finite values are taken (finite(), above), and
+// add_special then gives the others to the lanes that see them.
+template <int D>
+__device__ __forceinline__ void add_rows_finite(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
+                                                int first, bf16x8 b, unsigned &bad) {
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) acc[t] = mfma(finite(at.columns(tile, first, t), bad), b, acc[t]);
+}
+
+// What add_rows_finite left out: rows row0 .. row1 - 1 of a matrix whose row r is at src +
+// r ld; sees(r): does the lane's row see it?  A probability times an infinity or a NaN is that
+// infinity or NaN (it is positive, however small); a score's gradient times one is a NaN, for
+// the score itself is then infinite or NaN (nan = true).
 template <int D, typename F>
-__device__ __forceinline__ void add_rows_seen(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
-                                              int first, bf16x8 b, F &&sees) {
-  bf16x8 a[D / 32];
-  bool bad = false;
+__device__ __forceinline__ void add_special(f32x16 (&acc)[D / 32], const __bf16 *src, int64_t ld, int dim, int row0,
+                                            int row1, bool nan, F &&sees) {
+  for (int r = row0; r < row1; ++r) {
+    if (!sees(r)) continue;
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t) {
-    a[t] = at.columns(tile, first, t);
-    bad |= not_finite(a[t]);
-  }
-  if (!__any(bad)) {
+    for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) acc[t] = mfma(a[t], b, acc[t]);
-    return;
-  }
-  const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll 1
-  for (int c = 0; c < 16; ++c) {
-    const int e = h == ((c >> 2) & 1) ? (c >> 3) * 4 + (c & 3) : 8;
-    const bool keep = sees(c);
-    bf16x8 one;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) one[k] = k == e ? b[k] : (__bf16)0.f;
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t) {
-      bf16x8 row;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) row[k] = k == e ? a[t][k] : (__bf16)0.f;
-      f32x16 z;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = 0.f;
-      z = mfma(row, one, z);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][i] = keep ? acc[t][i] + z[i] : acc[t][i];
-    }
+      for (int i = 0; i < 16; ++i) {
+        const int col = 32 * t + 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4;
+        const float v = col < dim ? float(src[r * ld + col]) : 0.f;
+        if (!(fabsf(v) < INFINITY)) acc[t][i] += nan ? NAN : v;
+      }
   }
 }
 
 // row of D value i of 32: 8 (i / 4) + 4 (lane / 32) + i % 4
 __device__ __forceinline__ int d_row(int i) { return 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4; }
+
+// Tiles [0, n) through two places in LDS, as step(tile, place, masked) with place and masked constants:
+// the first `n1` of one kind (masked = FIRST), the others of the other, each kind's steps a loop of
+// their own without branches around them, which keeps the accumulators in their registers.  The
+// kind that tests every score serves any tile, so it takes the odd one.
+template <bool FIRST, typename F>
+__device__ __forceinline__ void two_kinds(int n, int n1, F &&step) {
+  using std::integral_constant;
+  const int even = FIRST ? min(n, n1 + (n1 & 1)) : n1 & ~1;
+  constexpr integral_constant<bool, FIRST> a{};
+  constexpr integral_constant<bool, !FIRST> b{};
+  constexpr integral_constant<int, 0> p0{};
+  constexpr integral_constant<int, 1> p1{};
+  int it = 0;
+  for (; it + 1 < even; it += 2) {
+    step(it, p0, a);
+    step(it + 1, p1, a);
+  }
+  if constexpr (FIRST) {
+    if (it < even) {  // n is odd, and all of it of this kind
+      step(it, p0, a);
+      return;
+    }
+  }
+  for (; it < n; it += 2) {
+    step(it, p0, b);
+    if (it + 1 < n) step(it + 1, p1, b);
+  }
+}
 
 // an accumulator's column, scaled, to a row of 16-bit values
 template <int D>
@@ -234,6 +299,19 @@ __device__ __forceinline__ void store_row(__bf16 *row, const f32x16 (&acc)[D / 3
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[t][4 * b + k] * scale);
       *reinterpret_cast<bf16x4 *>(row + col) = v;
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[D / 32], float scale, int dim) {
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
+      if (col < dim)
+        *reinterpret_cast<float4 *>(row + col) = make_float4(acc[t][4 * b] * scale, acc[t][4 * b + 1] * scale,
+                                                             acc[t][4 * b + 2] * scale, acc[t][4 * b + 3] * scale);
     }
 }
 

@@ -12,7 +12,8 @@ namespace {
 
 using namespace at;
 
-// sixteen lanes a row, eight columns each
+// delta, and lse in base 2 (infinite for rows that see nothing, so that p = exp2(-inf)); sixteen
+// lanes a row, eight columns each
 __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs A) {
   const int64_t at = blockIdx.x * int64_t(16) + threadIdx.x / 16;
   if (at >= A.heads * A.tq) return;
@@ -30,7 +31,11 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs A) {
   s = xor_add<2>(s);
   s = xor_add<4>(s);
   s = xor_add<8>(s);
-  if (col == 0) A.delta[head * A.tq + token] = s;
+  if (col == 0) {
+    const float lse = A.lse[head * A.tq + token];
+    A.delta[head * A.tq + token] = s;
+    A.lse2[head * A.tq + token] = lse == -INFINITY ? INFINITY : lse * LOG2E;
+  }
 }
 
 template <int D>
@@ -62,64 +67,64 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
       g[kk] = kept(pg, kk, A.dim);
     }
   }
-  const float lse2 = A.lse[head * A.tq + sq.q0 + token] * LOG2E, delta = A.delta[head * A.tq + sq.q0 + token];
-  const Places<D> at;
-  const __bf16 *const kp = A.k + sq.k0 * A.ldk + kvh * A.hsk, *const vp = A.v + sq.k0 * A.ldv + kvh * A.hsv;
-  auto load = [&](int it, unsigned char *kt, unsigned char *vt) {
-    load_tile<D, BN, 256>(kt, kp + int64_t(it) * BN * A.ldk, A.ldk, sq.lk - it * BN, A.dim);
-    load_tile<D, BN, 256>(vt, vp + int64_t(it) * BN * A.ldv, A.ldv, sq.lk - it * BN, A.dim);
+  const float lse2 = A.lse2[head * A.tq + sq.q0 + token], delta = A.delta[head * A.tq + sq.q0 + token];
+  const Places<D> places;
+  const __bf16 *const kp = A.k + sq.k0 * A.ldk + kvh * A.hsk;
+  const Loader<D, BN, 256> kload(kp, A.ldk, A.dim), vload(A.v + sq.k0 * A.ldv + kvh * A.hsv, A.ldv, A.dim);
+  auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+    kload.load(kt, int64_t(it) * BN, sq.lk - it * BN);
+    vload.load(vt, int64_t(it) * BN, sq.lk - it * BN);
   };
+  unsigned bad = 0;
   f32x16 dq[T];
   clear(dq);
   const float sc = A.scale * LOG2E;
 
-  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) {
+  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
+    const Places<D> at = places.here();
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
       f32x16 s[1], dp[1];
       clear(s);
       clear(dp);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        s[0] = mfma(at.rows(kt, u * 32, kk), q[kk], s[0]);
-        dp[0] = mfma(at.rows(vt, u * 32, kk), g[kk], dp[0]);
-      }
+      in_turn<2 * KK, 4>([&](int i) { return at.rows(i & 1 ? vt : kt, u * 32, i / 2); },
+                         [&](int i, bf16x8 a) {
+                           if (i & 1) dp[0] = mfma(a, g[i / 2], dp[0]);
+                           else s[0] = mfma(a, q[i / 2], s[0]);
+                         });
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = exp2_fast(fmaf(s[0][i], sc, -lse2)), ds = p * (dp[0][i] - delta);
         s[0][i] = MASKED && it * BN + u * 32 + d_row(i) >= lim ? 0.f : ds;
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int first = u * 32 + c * 16;
-        if constexpr (MASKED)
-          add_rows_seen<D>(dq, at, kt, first, operand(s[0], c), [&](int k) { return it * BN + first + k < lim; });
-        else
-          add_rows<D>(dq, at, kt, first, operand(s[0], c));
-      }
+      const bf16x8 ds[2] = {operand(s[0], 0), operand(s[0], 1)};
+      in_turn<2 * T, 4>([&](int i) { return at.columns(kt, u * 32 + i / T * 16, i % T); },
+                        [&](int i, bf16x8 a) { dq[i % T] = mfma(MASKED ? finite(a, bad) : a, ds[i / T], dq[i % T]); });
     }
   };
-  auto step = [&](int it, const unsigned char *kt, const unsigned char *vt, unsigned char *kn, unsigned char *vn) {
-    tile_barrier();
-    if (it + 1 < end) load(it + 1, kn, vn);
-    if (it * BN >= lim_hi) return;
-    if (it * BN + BN > lim_lo) work(it, kt, vt, std::true_type());
-    else work(it, kt, vt, std::false_type());
-  };
   if (end > 0) load(0, kt0, vt0);
-  for (int it = 0; it < end; it += 2) {
-    step(it, kt0, vt0, kt1, vt1);
-    if (it + 1 < end) step(it + 1, kt1, vt1, kt0, vt0);
-  }
+  two_kinds<false>(end, min(end, lim_lo / BN), [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+    tile_barrier();
+    if (it + 1 < end) load(it + 1, place ? kt0 : kt1, place ? vt0 : vt1);
+    work(it, place ? kt1 : kt0, place ? vt1 : vt0, masked);
+  });
+  if (__any(bad != 0))
+    add_special<D>(dq, kp, A.ldk, A.dim, lim_lo / BN * BN, lim_hi, true, [&](int j) { return j < lim; });
   if (valid) store_row<D>(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
 }
 
+static __device__ __align__(16) const float g_infinity[64] = {
+#define CKPT_INF4 INFINITY, INFINITY, INFINITY, INFINITY
+#define CKPT_INF16 CKPT_INF4, CKPT_INF4, CKPT_INF4, CKPT_INF4
+    CKPT_INF16, CKPT_INF16, CKPT_INF16, CKPT_INF16};
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
-  constexpr int BM = 128, BN = 64, T = D / 32, KK = D / 16;
+  constexpr int BM = 128, BN = D == 128 ? 32 : 64, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char qt0[BN * D * 2], qt1[BN * D * 2], gt0[BN * D * 2], gt1[BN * D * 2];
-  __shared__ float st0[2 * BN], st1[2 * BN];  // lse in base 2 | delta
+  __shared__ __align__(16) unsigned char vt[BM * D * 2];
+  __shared__ __align__(16) float st0[128], st1[128];  // lse in base 2 | delta, 64 places each
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
   Sequence sq;
@@ -131,100 +136,159 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   const int from = A.causal ? max(0, key - past) : 0;
   const int from_lo = __builtin_amdgcn_readfirstlane(from), from_hi = __builtin_amdgcn_readlane(from, 31);
   const int begin = (A.causal ? max(0, first - past) : 0) / BN, end = (sq.lq + BN - 1) / BN;
-  const int per = max(0, end - begin), n = per * A.rep;  // tiles of a head, of all
+  const int heads = A.rep / A.parts, head0 = kvh * A.rep + int(blockIdx.y) * heads;
+  const int per = max(0, end - begin), n = per * heads;  // tiles of a head, of all
 
-  bf16x8 k[KK], v[KK];
+  bf16x8 k[KK];
   {
-    const int kr = min(key, sq.lk - 1);
-    const __bf16 *p = A.k + (sq.k0 + kr) * A.ldk + kvh * A.hsk, *pv = A.v + (sq.k0 + kr) * A.ldv + kvh * A.hsv;
+    const __bf16 *p = A.k + (sq.k0 + min(key, sq.lk - 1)) * A.ldk + kvh * A.hsk;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      k[kk] = kept(p, kk, A.dim);
-      v[kk] = kept(pv, kk, A.dim);
-    }
+    for (int kk = 0; kk < KK; ++kk) k[kk] = kept(p, kk, A.dim);
   }
-  const Places<D> at;
+  const Places<D> places;
   const float sc = A.scale * LOG2E;
-  auto load = [&](int it, unsigned char *qt, unsigned char *gt, float *st) {
-    const int head = kvh * A.rep + it / per, t0 = (begin + it % per) * BN;
-    load_tile<D, BN, 256>(qt, A.q + (sq.q0 + t0) * A.ldq + head * A.hsq, A.ldq, sq.lq - t0, A.dim);
-    load_tile<D, BN, 256>(gt, A.g + (sq.q0 + t0) * A.ldo + head * A.hso, A.ldo, sq.lq - t0, A.dim);
-    if (threadIdx.x < BN) {
-      // rows past the sequence's and rows that see nothing: p = exp(-inf)
-      const int t = t0 + threadIdx.x;
-      const int64_t e = head * A.tq + sq.q0 + min(t, sq.lq - 1);
-      const float lse = A.lse[e];
-      st[threadIdx.x] = t < sq.lq && lse != -INFINITY ? lse * LOG2E : INFINITY;
-      st[BN + threadIdx.x] = t < sq.lq && lse != -INFINITY ? A.delta[e] : 0.f;
+  const Loader<D, BN, 256> qload(A.q + sq.q0 * A.ldq + head0 * A.hsq, A.ldq, A.dim),
+      gload(A.g + sq.q0 * A.ldo + head0 * A.hso, A.ldo, A.dim);
+  auto load = [&](int h, int t, unsigned char *qt, unsigned char *gt, float *st) __attribute__((always_inline)) {
+    const int t0 = t * BN;
+    qload.load(qt, t0, sq.lq - t0, h * A.hsq);
+    gload.load(gt, t0, sq.lq - t0, h * A.hso);
+    // a wavefront each; rows past the sequence's: p = exp2(-inf)
+    if (wave < 2) {
+      const bool ok = t0 + lane < sq.lq && lane < BN;
+      const int64_t e = (head0 + h) * A.tq + sq.q0 + t0 + lane;
+      const float *const none = wave ? reinterpret_cast<const float *>(g_zeros) + lane : g_infinity + lane;
+      const float *const p = ok ? (wave ? A.delta : A.lse2) + e : none;
+      __builtin_amdgcn_global_load_lds(p, (lds_void *)(st + 64 * wave), 4, 0, 0);
     }
   };
   f32x16 dk[T], dv[T];
   clear(dk);
   clear(dv);
+  unsigned badq = 0, badg = 0;
 
-  auto work = [&](int t0, const unsigned char *qt, const unsigned char *gt, const float *st, auto masked) {
+  auto work = [&](int t0, const unsigned char *qt, const unsigned char *gt, const float *st, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
+    const Places<D> at = places.here();
 #pragma unroll
     for (int u = 0; u < BN / 32; ++u) {
       f32x16 s[1], dp[1];
       clear(s);
       clear(dp);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        s[0] = mfma(at.rows(qt, u * 32, kk), k[kk], s[0]);
-        dp[0] = mfma(at.rows(gt, u * 32, kk), v[kk], dp[0]);
-      }
+      in_turn<KK, 4>([&](int i) { return at.rows(qt, u * 32, i); },
+                     [&](int i, bf16x8 a) { s[0] = mfma(a, k[i], s[0]); });
+      struct Pair {
+        bf16x8 g, v;
+      };
+      in_turn<KK, 2>([&](int i) { return Pair{at.rows(gt, u * 32, i), at.rows(vt, wave * 32, i)}; },
+                     [&](int i, const Pair &a) { dp[0] = mfma(a.g, a.v, dp[0]); });
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const int first = u * 32 + 8 * b + 4 * (lane >> 5);
-        const float4 ls = *reinterpret_cast<const float4 *>(st + first), de = *reinterpret_cast<const float4 *>(st + BN + first);
+        const int row = u * 32 + 8 * b + 4 * (lane >> 5);
+        const float4 ls = *reinterpret_cast<const float4 *>(st + row), de = *reinterpret_cast<const float4 *>(st + 64 + row);
         const float lsa[4] = {ls.x, ls.y, ls.z, ls.w}, dea[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * b + e;
-          const bool hidden = MASKED && t0 + first + e < from;
+          const bool hidden = MASKED && t0 + row + e < from;
           const float p = exp2_fast(fmaf(s[0][i], sc, -lsa[e])), ds = p * (dp[0][i] - dea[e]);
           s[0][i] = hidden ? 0.f : p;
           dp[0][i] = hidden ? 0.f : ds;
         }
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int first = u * 32 + c * 16;
-        if constexpr (MASKED) {
-          auto sees = [&](int r) { return t0 + first + r >= from; };
-          add_rows_seen<D>(dv, at, gt, first, operand(s[0], c), sees);
-          add_rows_seen<D>(dk, at, qt, first, operand(dp[0], c), sees);
-        } else {
-          add_rows<D>(dv, at, gt, first, operand(s[0], c));
-          add_rows<D>(dk, at, qt, first, operand(dp[0], c));
-        }
+      const bf16x8 pb[2] = {operand(s[0], 0), operand(s[0], 1)}, ds[2] = {operand(dp[0], 0), operand(dp[0], 1)};
+      in_turn<2 * T, 4>([&](int i) { return at.columns(gt, u * 32 + i / T * 16, i % T); },
+                        [&](int i, bf16x8 a) { dv[i % T] = mfma(MASKED ? finite(a, badg) : a, pb[i / T], dv[i % T]); });
+      in_turn<2 * T, 4>([&](int i) { return at.columns(qt, u * 32 + i / T * 16, i % T); },
+                        [&](int i, bf16x8 a) { dk[i % T] = mfma(MASKED ? finite(a, badq) : a, ds[i / T], dk[i % T]); });
+    }
+  };
+  // the tiles that hold queries before some key's first, of all heads, then the others
+  const int seen = min(end, max(begin, A.causal ? (max(0, min(first + BM, sq.lk) - 1 - past) + BN - 1) / BN : 0));
+  int h = 0, t = seen > begin ? begin : seen;  // of the next tile to load
+  bool late = seen == begin;
+  auto next = [&](unsigned char *qt, unsigned char *gt, float *st) __attribute__((always_inline)) {
+    load(h, t, qt, gt, st);
+    if (++t == (late ? end : seen)) {
+      t = late ? seen : begin;
+      if (++h == heads) {
+        late = true;
+        h = 0;
+        t = seen;
       }
     }
   };
-  auto step = [&](int it, const unsigned char *qt, const unsigned char *gt, const float *st, unsigned char *qn,
-                  unsigned char *gn, float *sn) {
-    tile_barrier();
-    if (it + 1 < n) load(it + 1, qn, gn, sn);
-    const int t0 = (begin + it % per) * BN;
-    if (t0 + BN <= from_lo) return;
-    if (t0 < from_hi) work(t0, qt, gt, st, std::true_type());
-    else work(t0, qt, gt, st, std::false_type());
-  };
-  if (n > 0) load(0, qt0, gt0, st0);
-  for (int it = 0; it < n; it += 2) {
-    step(it, qt0, gt0, st0, qt1, gt1, st1);
-    if (it + 1 < n) step(it + 1, qt1, gt1, st1, qt0, gt0, st0);
+  if (n > 0) {
+    Loader<D, BM, 256>(A.v + sq.k0 * A.ldv + kvh * A.hsv, A.ldv, A.dim).load(vt, first, sq.lk - first);
+    next(qt0, gt0, st0);
   }
+  int wt = seen > begin ? begin : seen;  // the tile that is worked on
+  bool wlate = seen == begin;
+  int wh = 0;
+  two_kinds<true>(n, (seen - begin) * heads, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+    tile_barrier();
+    if (it + 1 < n) next(place ? qt0 : qt1, place ? gt0 : gt1, place ? st0 : st1);
+    work(wt * BN, place ? qt1 : qt0, place ? gt1 : gt0, place ? st1 : st0, masked);
+    if (++wt == (wlate ? end : seen)) {
+      wt = wlate ? seen : begin;
+      if (++wh == heads) {
+        wlate = true;
+        wt = seen;
+      }
+    }
+  });
+  if (__any((badq | badg) != 0))
+    for (h = 0; h < heads; ++h) {
+      auto sees = [&](int r) { return r >= from; };
+      const int row1 = min(sq.lq, (from_hi + BN - 1) / BN * BN), row0 = min(row1, from_lo / BN * BN);
+      add_special<D>(dv, A.g + sq.q0 * A.ldo + (head0 + h) * A.hso, A.ldo, A.dim, row0, row1, false, sees);
+      add_special<D>(dk, A.q + sq.q0 * A.ldq + (head0 + h) * A.hsq, A.ldq, A.dim, row0, row1, true, sees);
+    }
   if (!valid) return;
+  if (A.parts > 1) {
+    // fp32, for k_attn_heads: dk's parts, then dv's
+    float *const p = A.pkv + ((int64_t(blockIdx.y) * A.tk + sq.k0 + key) * A.kv_heads + kvh) * A.dim;
+    store_part<D>(p, dk, A.scale, A.dim);
+    store_part<D>(p + A.parts * A.tk * A.kv_heads * A.dim, dv, 1.f, A.dim);
+    return;
+  }
   store_row<D>(A.dk + (sq.k0 + key) * A.ldk + kvh * A.hsk, dk, A.scale, A.dim);
   store_row<D>(A.dv + (sq.k0 + key) * A.ldv + kvh * A.hsv, dv, 1.f, A.dim);
+}
+
+// the parts of the query heads that share a key head, added up in order; a thread has eight columns
+// of dk (blockIdx.y 0) or dv
+__global__ __launch_bounds__(256) void k_attn_heads(AttnArgs A) {
+  const int vecs = A.dim / 8;
+  const int64_t at = blockIdx.x * int64_t(256) + threadIdx.x, row = at / vecs, n = A.tk * A.kv_heads;
+  if (row >= n) return;
+  const int64_t token = row / A.kv_heads;
+  if (token < A.koff[0] || token >= A.koff[A.seqs]) return;
+  const int head = int(row - token * A.kv_heads), col = int(at - row * vecs) * 8;
+  const float *p = A.pkv + ((blockIdx.y ? int64_t(A.parts) * n : 0) + row) * A.dim + col;
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int k = 0; k < A.parts; ++k, p += n * A.dim) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w;
+    s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
+  }
+  bf16x8 r;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) r[k] = (__bf16)s[k];
+  __bf16 *const to = blockIdx.y ? A.dv + token * A.ldv + head * A.hsv : A.dk + token * A.ldk + head * A.hsk;
+  *reinterpret_cast<bf16x8 *>(to + col) = r;
 }
 
 template <int D>
 void backward(hipStream_t s, const AttnArgs &a) {
   const int kt = int(a.tk / 128) + a.seqs, qt = int(a.tq * a.rep / 128) + a.seqs;
-  if (a.tk > 0) hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads), dim3(256), 0, s, a);
+  if (a.tk > 0) {
+    hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads, a.parts), dim3(256), 0, s, a);
+    if (a.parts > 1)
+      hipLaunchKernelGGL(k_attn_heads, dim3(uint32_t((a.tk * a.kv_heads * (a.dim / 8) + 255) / 256), 2), dim3(256), 0, s,
+                         a);
+  }
   if (a.tq > 0) hipLaunchKernelGGL(k_attn_dq<D>, dim3(uint32_t(qt) * a.kv_heads), dim3(256), 0, s, a, qt);
 }
 
@@ -232,19 +296,35 @@ void backward(hipStream_t s, const AttnArgs &a) {
 
 int attn_splits(const AttnArgs &a);
 
+// Workgroups that a key head's query heads are dealt to, a divisor of their number: as many as
+// make two workgroups for each place on the chip, so that the causal ones, of all lengths, even out.
+static int parts_of(const AttnArgs &a) {
+  const int64_t work = (a.tk / 128 > a.seqs ? a.tk / 128 : a.seqs) * a.kv_heads;
+  int n = 1;
+  while (n < a.rep && (a.rep % n || work * n < 1024)) ++n;
+  return n;
+}
+
 uint64_t attn_plan(AttnArgs &a, bool backward, char *ws) {
+  auto align4 = [](uint64_t v) { return (v + 3) / 4 * 4; };
   if (backward) {
-    if (ws) a.delta = reinterpret_cast<float *>(ws);
-    return 4 * uint64_t(a.heads) * a.tq;
+    a.parts = parts_of(a);
+    const uint64_t rows = align4(uint64_t(a.heads) * a.tq);
+    if (ws) {
+      a.delta = reinterpret_cast<float *>(ws);
+      a.lse2 = a.delta + rows;
+      a.pkv = a.lse2 + rows;
+    }
+    return 4 * (2 * rows + (a.parts > 1 ? 2 * uint64_t(a.parts) * a.tk * a.kv_heads * a.dim : 0));
   }
   a.splits = attn_splits(a);
   if (a.splits == 1) return 0;
   const uint64_t rows = uint64_t(a.splits) * a.heads * a.tq;
   if (ws) {
     a.pml = reinterpret_cast<float *>(ws);
-    a.po = a.pml + (2 * rows + 3) / 4 * 4;
+    a.po = a.pml + align4(2 * rows);
   }
-  return 4 * ((2 * rows + 3) / 4 * 4 + rows * a.dim);
+  return 4 * (align4(2 * rows) + rows * a.dim);
 }
 
 void attn_backward(hipStream_t s, const AttnArgs &a) {

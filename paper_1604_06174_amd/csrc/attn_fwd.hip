@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
   const int token = int(r / A.rep), head = kvh * A.rep + int(r - int64_t(token) * A.rep);
   const int past = sq.lk - sq.lq;
   const int lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;  // keys it sees
-  const int lim_lo = __builtin_amdgcn_readfirstlane(lim), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+  const int lim_lo = __builtin_amdgcn_readfirstlane(lim), lim_hi = __builtin_amdgcn_readlane(lim, 31);  // the wavefront's least and most
   const int64_t last = min(sq.first + BM, rows) - 1;
   const int kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
   const int all = (kend + BN - 1) / BN;
@@ -48,20 +48,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
   }
-  const Places<D> at;
-  const __bf16 *const kp = A.k + sq.k0 * A.ldk + kvh * A.hsk, *const vp = A.v + sq.k0 * A.ldv + kvh * A.hsv;
-  auto load = [&](int it, unsigned char *kt, unsigned char *vt) {
-    load_tile<D, BN, 256>(kt, kp + int64_t(it) * BN * A.ldk, A.ldk, sq.lk - it * BN, A.dim);
-    load_tile<D, BN, 256>(vt, vp + int64_t(it) * BN * A.ldv, A.ldv, sq.lk - it * BN, A.dim);
-  };
+  const Places<D> places;
+  const __bf16 *const vp = A.v + sq.k0 * A.ldv + kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
 
   f32x16 o[T];
   clear(o);
   float m = -INFINITY, l = 0.f;
   const float sc = A.scale * LOG2E;
+  unsigned bad = 0;
 
-  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) {
+  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
+    const Places<D> at = places.here();
     const int j0 = it * BN + wk * SUBS * 32;  // the wavefront's first key
     f32x16 s[SUBS];
     clear(s);
@@ -77,8 +76,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
         if (MASKED && j0 + u * 32 + d_row(i) >= lim) s[u][i] = -INFINITY;
         top = fmaxf(top, s[u][i]);
       }
-    top = fmaxf(m, halves_max(top));
-    if (__any(top > m)) {
+    top = halves_max(top);
+    // The maximum is moved when it would let an exponential exceed 2^8: o and l stay far
+    // inside fp32, and most tiles leave them as they are.
+    if (__any((top - m) * sc > 8.f)) {
+      top = fmaxf(m, top);
       const float f = exp2_fast((m - (top == -INFINITY ? 0.f : top)) * sc);
       m = top;
       l *= f;
@@ -100,25 +102,30 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int first = (wk * SUBS + u) * 32 + c * 16;
-        if constexpr (MASKED)
-          add_rows_seen<D>(o, at, vt, first, operand(s[u], c), [&](int k) { return it * BN + first + k < lim; });
-        else
-          add_rows<D>(o, at, vt, first, operand(s[u], c));
+        if constexpr (MASKED) add_rows_finite<D>(o, at, vt, first, operand(s[u], c), bad);
+        else add_rows<D>(o, at, vt, first, operand(s[u], c));
       }
   };
-  auto step = [&](int it, const unsigned char *kt, const unsigned char *vt, unsigned char *kn, unsigned char *vn) {
-    tile_barrier();
-    if (it + 1 < end) load(it + 1, kn, vn);
-    const int j0 = it * BN + wk * SUBS * 32;
-    if (j0 >= lim_hi) return;
-    if (j0 + SUBS * 32 > lim_lo) work(it, kt, vt, std::true_type());
-    else work(it, kt, vt, std::false_type());
+  const int n = end - begin;
+  // tiles whose keys every row of the wavefront sees
+  const int whole = lim_lo - (wk + 1) * SUBS * 32 + BN;
+  const int full = max(0, min(n, (whole > 0 ? whole / BN : 0) - begin));
+  auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+    kload.load(kt, int64_t(it) * BN, sq.lk - it * BN);
+    vload.load(vt, int64_t(it) * BN, sq.lk - it * BN);
   };
-  if (begin < end) load(begin, kt0, vt0);
-  for (int it = begin; it < end; it += 2) {
-    step(it, kt0, vt0, kt1, vt1);
-    if (it + 1 < end) step(it + 1, kt1, vt1, kt0, vt0);
-  }
+  if (n > 0) load(begin, kt0, vt0);
+  two_kinds<false>(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
+    tile_barrier();
+    if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
+    work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
+  });
+  if (__any(bad != 0))
+    for (int it = begin; it < end; ++it) {
+      const int j0 = it * BN + wk * SUBS * 32;
+      if (j0 + SUBS * 32 > lim_lo && j0 < lim_hi)
+        add_special<D>(o, vp, A.ldv, A.dim, j0, min(j0 + SUBS * 32, sq.lk), false, [&](int j) { return j < lim; });
+    }
   l = halves_add(l);
 
   if constexpr (WK > 1) {
@@ -164,16 +171,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
       A.pml[2 * p] = m;
       A.pml[2 * p + 1] = l;
     }
-    float *const out = A.po + p * A.dim;
-#pragma unroll
-    for (int t = 0; t < T; ++t)
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int col = 32 * t + 8 * b + 4 * (lane >> 5);
-        if (col < A.dim)
-          *reinterpret_cast<float4 *>(out + col) =
-              make_float4(o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]);
-      }
+    store_part<D>(A.po + p * A.dim, o, 1.f, A.dim);
     return;
   }
   if (lane < 32) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(m, A.scale, logf(l));

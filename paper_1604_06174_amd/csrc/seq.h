@@ -65,7 +65,9 @@ struct AttnArgs {
   // backward
   const __bf16 *g, *out;
   __bf16 *dq, *dk, *dv;
-  float *delta;  // [heads, tq] sums of g o
+  float *delta, *lse2;  // [heads, tq] sums of g o; lse in base 2
+  int parts;            // workgroups that share a key head's query heads
+  float *pkv;           // [2][parts][tk][kv_heads][dim] their dk and dv, if more than one
   int64_t tq, tk;
   int64_t ldq, hsq, ldk, hsk, ldv, hsv, ldo, hso;
   int seqs, heads, kv_heads, rep, dim, causal;  // rep: heads / kv_heads
