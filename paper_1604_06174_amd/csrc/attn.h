@@ -128,29 +128,22 @@ struct Loader {
 // a lane's places in a tile: of its row's chunks, and of the transposing reads
 template <int D>
 struct Places {
-  int row;  // byte offset of chunk lane / 32 of row lane % 32; chunk 2 kk further on: ^ kk << 5
-  int lo[D / 32], hi[D / 32];
+  int row;     // byte offset of chunk lane / 32 of row lane % 32; chunk 2 kk further on: ^ kk << 5
+  int lo, hi;  // of the transposing reads of columns 0 .. 31; 32 b columns further on: ^ b << 6
 
   __device__ __forceinline__ Places() {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     row = r * D * 2 + ((swizzle<D>(r) ^ h) << 4);
-    const int t = (lane >> 2) & 3;
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) {
-      const int chunk = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      const int r0 = 4 * h + t, r1 = r0 + 8;
-      lo[b] = r0 * D * 2 + ((chunk ^ swizzle<D>(r0)) << 4) + (lane & 1) * 8;
-      hi[b] = r1 * D * 2 + ((chunk ^ swizzle<D>(r1)) << 4) + (lane & 1) * 8;
-    }
+    const int chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), r0 = 4 * h + ((lane >> 2) & 3), r1 = r0 + 8;
+    lo = r0 * D * 2 + ((chunk ^ swizzle<D>(r0)) << 4) + (lane & 1) * 8;
+    hi = r1 * D * 2 + ((chunk ^ swizzle<D>(r1)) << 4) + (lane & 1) * 8;
   }
   // A copy that the compiler takes for new values.  A tile's address in LDS is then an offset
   // within the reads; otherwise its sum with every place is formed before the loop, and
   // four tiles' sums take the registers of an accumulator.
   __device__ __forceinline__ Places here() const {
     Places p = *this;
-    asm volatile("" : "+v"(p.row));
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) asm volatile("" : "+v"(p.lo[b]), "+v"(p.hi[b]));
+    asm volatile("" : "+v"(p.row), "+v"(p.lo), "+v"(p.hi));
     return p;
   }
 
@@ -160,8 +153,8 @@ struct Places {
   }
   // A transposed: m = columns 32 b .. 32 b + 31, k = the 16 rows from `first` (a multiple of 16) on
   __device__ __forceinline__ bf16x8 columns(const unsigned char *tile, int first, int b) const {
-    const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + lo[b]));
-    const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + hi[b]));
+    const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + (lo ^ (b << 6))));
+    const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(tile + first * D * 2 + (hi ^ (b << 6))));
     const short8v v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     return __builtin_bit_cast(bf16x8, v);
   }
@@ -212,6 +205,8 @@ __device__ __forceinline__ bf16x8 finite(bf16x8 a, unsigned &bad) {
     bad |= f ^ w[k];
     w[k] = f;
   }
+  // here and now: added up at a block's end, these would keep all the values until then
+  asm volatile("" : "+v"(bad));
   return __builtin_bit_cast(bf16x8, w);
 }
 
@@ -257,31 +252,22 @@ __device__ __forceinline__ void add_special(f32x16 (&acc)[D / 32], const __bf16 
 __device__ __forceinline__ int d_row(int i) { return 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4; }
 
 // Tiles [0, n) through two places in LDS, as step(tile, place, masked) with place and masked constants:
-// the first `n1` of one kind (masked = FIRST), the others of the other, each kind's steps a loop of
-// their own without branches around them, which keeps the accumulators in their registers.  The
-// kind that tests every score serves any tile, so it takes the odd one.
-template <bool FIRST, typename F>
+// the first `n1` without tests of every score, the others with.  Each kind's steps are a loop
+// of their own without branches around them, which keeps the accumulators in their registers;
+// the kind with tests serves any tile, so it takes an odd one too.
+template <typename F>
 __device__ __forceinline__ void two_kinds(int n, int n1, F &&step) {
   using std::integral_constant;
-  const int even = FIRST ? min(n, n1 + (n1 & 1)) : n1 & ~1;
-  constexpr integral_constant<bool, FIRST> a{};
-  constexpr integral_constant<bool, !FIRST> b{};
   constexpr integral_constant<int, 0> p0{};
   constexpr integral_constant<int, 1> p1{};
   int it = 0;
-  for (; it + 1 < even; it += 2) {
-    step(it, p0, a);
-    step(it + 1, p1, a);
-  }
-  if constexpr (FIRST) {
-    if (it < even) {  // n is odd, and all of it of this kind
-      step(it, p0, a);
-      return;
-    }
+  for (; it + 1 < n1; it += 2) {
+    step(it, p0, std::false_type());
+    step(it + 1, p1, std::false_type());
   }
   for (; it < n; it += 2) {
-    step(it, p0, b);
-    if (it + 1 < n) step(it + 1, p1, b);
+    step(it, p0, std::true_type());
+    if (it + 1 < n) step(it + 1, p1, std::true_type());
   }
 }
 

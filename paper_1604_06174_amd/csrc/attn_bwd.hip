@@ -83,6 +83,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const Places<D> at = places.here();
+    const int left = lim - it * BN - 4 * (lane >> 5);  // keys the lane's query sees from its half's first on
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
       f32x16 s[1], dp[1];
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = exp2_fast(fmaf(s[0][i], sc, -lse2)), ds = p * (dp[0][i] - delta);
-        s[0][i] = MASKED && it * BN + u * 32 + d_row(i) >= lim ? 0.f : ds;
+        s[0][i] = MASKED && u * 32 + 8 * (i / 4) + i % 4 >= left ? 0.f : ds;
       }
       const bf16x8 ds[2] = {operand(s[0], 0), operand(s[0], 1)};
       in_turn<2 * T, 4>([&](int i) { return at.columns(kt, u * 32 + i / T * 16, i % T); },
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
     }
   };
   if (end > 0) load(0, kt0, vt0);
-  two_kinds<false>(end, min(end, lim_lo / BN), [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+  two_kinds(end, min(end, lim_lo / BN), [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
     if (it + 1 < end) load(it + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(it, place ? kt1 : kt0, place ? vt1 : vt0, masked);
@@ -170,6 +171,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   auto work = [&](int t0, const unsigned char *qt, const unsigned char *gt, const float *st, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const Places<D> at = places.here();
+    const int unseen = from - t0 - 4 * (lane >> 5);  // queries that do not see the lane's key, from its half's first on
 #pragma unroll
     for (int u = 0; u < BN / 32; ++u) {
       f32x16 s[1], dp[1];
@@ -190,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * b + e;
-          const bool hidden = MASKED && t0 + row + e < from;
+          const bool hidden = MASKED && u * 32 + 8 * b + e < unseen;
           const float p = exp2_fast(fmaf(s[0][i], sc, -lsa[e])), ds = p * (dp[0][i] - dea[e]);
           s[0][i] = hidden ? 0.f : p;
           dp[0][i] = hidden ? 0.f : ds;
@@ -203,42 +205,36 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
                         [&](int i, bf16x8 a) { dk[i % T] = mfma(MASKED ? finite(a, badq) : a, ds[i / T], dk[i % T]); });
     }
   };
-  // the tiles that hold queries before some key's first, of all heads, then the others
+  // Tiles from the last query back: workgroups that start together read the same tiles together
+  // (through one L2), and the tiles with queries before some key's first come last, after all heads'
+  // others.
   const int seen = min(end, max(begin, A.causal ? (max(0, min(first + BM, sq.lk) - 1 - past) + BN - 1) / BN : 0));
-  int h = 0, t = seen > begin ? begin : seen;  // of the next tile to load
-  bool late = seen == begin;
+  struct Cursor {
+    int h, t, lo, hi;  // head, tile, its kind's tiles
+  };
+  auto advance = [&](Cursor &c) __attribute__((always_inline)) {
+    if (--c.t >= c.lo) return;
+    if (++c.h == heads) c = Cursor{0, 0, begin, seen};
+    c.t = c.hi - 1;
+  };
+  const Cursor start = seen < end ? Cursor{0, end - 1, seen, end} : Cursor{0, seen - 1, begin, seen};
+  Cursor ahead = start, now = start;
   auto next = [&](unsigned char *qt, unsigned char *gt, float *st) __attribute__((always_inline)) {
-    load(h, t, qt, gt, st);
-    if (++t == (late ? end : seen)) {
-      t = late ? seen : begin;
-      if (++h == heads) {
-        late = true;
-        h = 0;
-        t = seen;
-      }
-    }
+    load(ahead.h, ahead.t, qt, gt, st);
+    advance(ahead);
   };
   if (n > 0) {
     Loader<D, BM, 256>(A.v + sq.k0 * A.ldv + kvh * A.hsv, A.ldv, A.dim).load(vt, first, sq.lk - first);
     next(qt0, gt0, st0);
   }
-  int wt = seen > begin ? begin : seen;  // the tile that is worked on
-  bool wlate = seen == begin;
-  int wh = 0;
-  two_kinds<true>(n, (seen - begin) * heads, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+  two_kinds(n, (end - seen) * heads, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
     if (it + 1 < n) next(place ? qt0 : qt1, place ? gt0 : gt1, place ? st0 : st1);
-    work(wt * BN, place ? qt1 : qt0, place ? gt1 : gt0, place ? st1 : st0, masked);
-    if (++wt == (wlate ? end : seen)) {
-      wt = wlate ? seen : begin;
-      if (++wh == heads) {
-        wlate = true;
-        wt = seen;
-      }
-    }
+    work(now.t * BN, place ? qt1 : qt0, place ? gt1 : gt0, place ? st1 : st0, masked);
+    advance(now);
   });
   if (__any((badq | badg) != 0))
-    for (h = 0; h < heads; ++h) {
+    for (int h = 0; h < heads; ++h) {
       auto sees = [&](int r) { return r >= from; };
       const int row1 = min(sq.lq, (from_hi + BN - 1) / BN * BN), row0 = min(row1, from_lo / BN * BN);
       add_special<D>(dv, A.g + sq.q0 * A.ldo + (head0 + h) * A.hso, A.ldo, A.dim, row0, row1, false, sees);

@@ -61,7 +61,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
   auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const Places<D> at = places.here();
-    const int j0 = it * BN + wk * SUBS * 32;  // the wavefront's first key
+    // keys the lane's query sees from its half's first on
+    const int left = lim - (it * BN + wk * SUBS * 32) - 4 * (lane >> 5);
     f32x16 s[SUBS];
     clear(s);
 #pragma unroll
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
     for (int u = 0; u < SUBS; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        if (MASKED && j0 + u * 32 + d_row(i) >= lim) s[u][i] = -INFINITY;
+        if (MASKED && u * 32 + 8 * (i / 4) + i % 4 >= left) s[u][i] = -INFINITY;
         top = fmaxf(top, s[u][i]);
       }
     top = halves_max(top);
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
     vload.load(vt, int64_t(it) * BN, sq.lk - it * BN);
   };
   if (n > 0) load(begin, kt0, vt0);
-  two_kinds<false>(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
+  two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
     if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
