@@ -8,15 +8,19 @@
 //     wavefront, and places them.  The first position of a range is the number of
 //     smaller ids, which the workgroup counts as it goes, so workgroups need nothing of
 //     each other.
-//   k_embed_sum   a wavefront adds up the rows of a chunk of sorted positions, 512
-//     columns; an id whose tokens lie within the chunk is done, one that crosses an
-//     end leaves its part.  Other workgroups write the rows of absent ids.
-//   k_embed_join  adds the parts of an id that crosses chunks, in order.
+//   k_embed_sum   a wavefront takes a chunk of sorted positions, 512 columns, and adds up
+//     the ids that begin in it, up to their ends.  An id with more tokens than a chunk is taken in
+//     pieces of a chunk's length from its first on, each by the wavefront in whose chunk the
+//     piece begins, which leaves its sum.  The first workgroups write the rows of absent ids:
+//     their stores go out while the others look up what they have to add.
+//   k_embed_join  adds the pieces of such an id, in order.
 // Nothing is added by atomics (the counts are whole numbers), so the same bits come
 // out on every run.
 #include "common.h"
 #include "seq.h"
 #include "vec.h"
+
+#include <type_traits>
 
 namespace ckpt {
 namespace {
@@ -81,24 +85,64 @@ __global__ __launch_bounds__(256) void k_embed_forward(EmbedArgs A, int nvec, in
   }
 }
 
+// four ids from token i on as 32 bits: -1 for those past the end and for wide ones that 32 bits
+// do not hold (as unsigned numbers all of these lie above every vocabulary)
+template <bool WIDE>
+__device__ __forceinline__ void four_ids(const EmbedArgs &A, int64_t i, int64_t last, int id[4]) {
+  typedef typename std::conditional<WIDE, int64_t, int>::type I;
+  typedef I four __attribute__((ext_vector_type(4), aligned(sizeof(I))));
+  const I *const p = static_cast<const I *>(A.ids) + i;
+  four v = {-1, -1, -1, -1};
+  if (i + 4 <= last) {
+    v = *reinterpret_cast<const four *>(p);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u < last) v[u] = p[u];
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) id[u] = WIDE && (int64_t(v[u]) >> 31) ? -1 : int(v[u]);
+}
+
+// f(first token of 256, the lane's four ids) over tokens [first, last): 1024 tokens' ids are in
+// flight at once
+template <bool WIDE, typename F>
+__device__ __forceinline__ void each_ids(const EmbedArgs &A, int64_t first, int64_t last, F &&f) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t i = first; i < last; i += 1024) {
+    int id[4][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) four_ids<WIDE>(A, i + g * 256 + lane * 4, last, id[g]);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) f(i + g * 256, id[g]);
+  }
+}
+
+template <bool WIDE>
 __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int range) {
   __shared__ int cnt[SECTIONS * MAX_RANGE];  // [section][id of the range]
   __shared__ int wsum[SECTIONS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lo = int(min(int64_t(blockIdx.x) * range, A.vocab));
   const int n = int(min(int64_t(range), A.vocab - lo));
-  const int64_t per = ((A.tokens + SECTIONS - 1) / SECTIONS + 63) / 64 * 64;
+  const int64_t per = ((A.tokens + SECTIONS - 1) / SECTIONS + 255) / 256 * 256;
   const int64_t first = min(wave * per, A.tokens), last = min(first + per, A.tokens);
   for (int i = threadIdx.x; i < SECTIONS * range; i += 64 * SECTIONS) cnt[i] = 0;
   __syncthreads();
 
   int less = 0;
-#pragma unroll 4
-  for (int64_t i = first; i < last; i += 64) {
-    const int id = i + lane < last ? id_at(A, i + lane) : -1;
-    less += id >= 0 && id < lo;
-    if (id >= lo && id < lo + n) atomicAdd(&cnt[wave * range + id - lo], 1);
-  }
+  each_ids<WIDE>(A, first, last, [&](int64_t, const int (&id)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) less += unsigned(id[u]) < unsigned(lo);
+    unsigned nearest = ~0u;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) nearest = min(nearest, unsigned(id[u]) - unsigned(lo));
+    if (nearest < unsigned(n)) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (unsigned(id[u]) - unsigned(lo) < unsigned(n)) atomicAdd(&cnt[wave * range + id[u] - lo], 1);
+    }
+  });
 #pragma unroll
   for (int o = 32; o; o >>= 1) less += __shfl_xor(less, o);
   if (lane == 0) wsum[wave] = less;
@@ -109,12 +153,14 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   __syncthreads();  // wsum is written again below
 
   // cnt becomes the first position of each section's tokens of an id: an exclusive sum over
-  // the ids, then over the sections; a thread has range / threads consecutive ids
-  const int each = (range + 64 * SECTIONS - 1) / (64 * SECTIONS);  // 1
+  // the ids, then over the sections; a thread has one id
+  static_assert(MAX_RANGE <= 64 * SECTIONS, "an id a thread");
+  const int i0 = threadIdx.x;
   int mine = 0;
-  const int i0 = threadIdx.x * each;
-  for (int i = i0; i < min(i0 + each, n); ++i)
-    for (int k = 0; k < SECTIONS; ++k) mine += cnt[k * range + i];
+  if (i0 < n) {
+#pragma unroll
+    for (int k = 0; k < SECTIONS; ++k) mine += cnt[k * range + i0];
+  }
   int incl = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -125,11 +171,12 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   __syncthreads();
   int pos = base + incl - mine;
   for (int k = 0; k < wave; ++k) pos += wsum[k];
-  for (int i = i0; i < min(i0 + each, n); ++i) {
-    A.start[lo + i] = pos;
+  if (i0 < n) {
+    A.start[lo + i0] = pos;
+#pragma unroll
     for (int k = 0; k < SECTIONS; ++k) {
-      const int t = cnt[k * range + i];
-      cnt[k * range + i] = pos;
+      const int t = cnt[k * range + i0];
+      cnt[k * range + i0] = pos;
       pos += t;
     }
   }
@@ -141,24 +188,38 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   }
   __syncthreads();
 
-  for (int64_t i = first; i < last; i += 64) {
-    const int id = i + lane < last ? id_at(A, i + lane) : -1;
-    uint64_t left = __ballot(id >= lo && id < lo + n);
-    while (left) {
-      const int key = __shfl(id, __ffsll((unsigned long long)left) - 1);
-      const uint64_t same = __ballot(id == key);
+  each_ids<WIDE>(A, first, last, [&](int64_t i, const int (&id)[4]) {
+    bool in[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) in[u] = unsigned(id[u]) - unsigned(lo) < unsigned(n);
+    // the range's ids of these 256 tokens one after the other, each with all its tokens
+    while (const uint64_t left = __ballot(in[0] | in[1] | in[2] | in[3])) {
+      const int some = in[0] ? id[0] : in[1] ? id[1] : in[2] ? id[2] : id[3];
+      const int key = __builtin_amdgcn_readlane(some, __ffsll((unsigned long long)left) - 1);
+      const uint64_t below = (1ull << lane) - 1;
+      int rank = 0, count = 0;  // the id's tokens in lower lanes, and in all
+      bool same[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        same[u] = id[u] == key;
+        const uint64_t b = __ballot(same[u]);
+        rank += __popcll(b & below);
+        count += __popcll(b);
+        in[u] &= !same[u];
+      }
       // one wavefront's: its accesses are in order, and volatile keeps them in the code's
       volatile int *const at = &cnt[wave * range + key - lo];
-      const int p = *at;
-      if (id == key) {
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        A.perm[p + rank] = int(i + lane);
-        A.key[p + rank] = key;
-        if (rank == 0) *at = p + __popcll(same);
-      }
-      left &= ~same;
+      int p = *at + rank;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (same[u]) {
+          A.perm[p] = int(i + lane * 4 + u);
+          A.key[p] = key;
+          ++p;
+        }
+      if (lane == 63) *at = p - rank + count - (same[0] + same[1] + same[2] + same[3]);
     }
-  }
+  });
 }
 
 // row `v` of the gradient = the sum, or the sum added to it
@@ -176,102 +237,157 @@ __device__ __forceinline__ void put_row(const EmbedArgs &A, int v, int col, int 
   store8(p, cnt, s);
 }
 
-// Workgroups below `sums` add up chunks, a wavefront each; the others write the
-// absent ids' rows.
 template <typename GT, typename DT>
-__global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (int(blockIdx.x) >= sums) {
-    const int64_t rows = int64_t(gridDim.x - sums) * 4;
-    const int64_t nvec = (A.c + 7) / 8;
-    for (int64_t v = (blockIdx.x - sums) * int64_t(4) + wave; v < A.vocab; v += rows) {
-      if (A.start[v] != A.start[v + 1]) continue;
-      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int64_t j = lane; j < nvec; j += 64)
-        store8(static_cast<DT *>(A.dst) + v * A.ldd + j * 8, min(8, A.c - int(j) * 8), zero);
+__global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int zeros) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (int(blockIdx.x) < zeros) {  // 64 ids a wavefront
+    const int64_t v0 = (blockIdx.x * int64_t(4) + wave) * 64, v = v0 + lane;
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (uint64_t absent = __ballot(v < A.vocab && A.start[v] == A.start[v + 1]); absent; absent &= absent - 1) {
+      DT *const row = static_cast<DT *>(A.dst) + (v0 + __ffsll((unsigned long long)absent) - 1) * A.ldd;
+      for (int col = lane * 8; col < A.c; col += 512) store8(row + col, min(8, A.c - col), zero);
     }
     return;
   }
-  const int64_t unit = blockIdx.x * int64_t(4) + wave;
+  const int64_t unit = (blockIdx.x - zeros) * int64_t(4) + wave;
   const int64_t chunk = unit / tiles;
   if (chunk >= A.chunks) return;
   const int col = int(unit - chunk * tiles) * 512 + lane * 8, cnt = min(8, A.c - col);
-  const int total = A.start[A.vocab];
-  const int64_t p0 = chunk * A.chunk;
-  const int len = int(min(int64_t(A.chunk), total - p0));
-  if (len <= 0) return;
-  int tok = 0, key = -1;
-  if (lane < len) {
-    tok = A.perm[p0 + lane];
-    key = A.key[p0 + lane];
+  const int total = A.start[A.vocab], P = A.chunk, p0 = int(min(chunk * P, int64_t(total))), p1 = min(p0 + P, total);
+  if (p0 == p1) {
+    if (lane == 0) A.tail[chunk] = -1;
+    return;
   }
-  const bool before = p0 > 0 && A.key[p0 - 1] == __shfl(key, 0);
-  const bool after = p0 + len < total && A.key[p0 + len] == __shfl(key, len - 1);
-  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  bool head = before;  // the rows so far belong to an id that began before the chunk
-  for (int q = 0; q < len; q += 8) {
-    float v[8][8];
+  // all positions that may have to be added up here, while the ids at the chunk's ends are looked up
+  int tok[2] = {0, 0}, key[2] = {-1, -1};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int64_t row = __builtin_amdgcn_readlane(tok, min(q + u, len - 1));
-      if (cnt > 0) load8(static_cast<const GT *>(A.src) + row * A.lds + col, cnt, v[u]);
+  for (int u = 0; u < 2; ++u)
+    if (p0 + u * 64 + lane < total) {
+      tok[u] = A.perm[p0 + u * 64 + lane];
+      key[u] = A.key[p0 + u * 64 + lane];
     }
+  auto token_at = [&](int q) { return q < 64 ? __builtin_amdgcn_readlane(tok[0], q) : __builtin_amdgcn_readlane(tok[1], q - 64); };
+  auto key_at = [&](int q) { return q < 64 ? __builtin_amdgcn_readlane(key[0], q) : __builtin_amdgcn_readlane(key[1], q - 64); };
+  const int k0 = key_at(0), k1 = key_at(p1 - p0 - 1);
+  const int begin0 = A.start[k0], end0 = A.start[k0 + 1], begin1 = A.start[k1], end1 = A.start[k1 + 1];
+  const bool long0 = end0 - begin0 > P, long1 = end1 - begin1 > P;
+  // the first id or piece that begins in the chunk, and the end of the last
+  int from = p0;
+  if (begin0 < p0) {
+    const int piece = begin0 + (p0 - begin0 + P - 1) / P * P;
+    from = min(p1, long0 && piece < end0 ? piece : end0);
+  }
+  const int last = long1 ? begin1 + (p1 - 1 - begin1) / P * P : begin1;
+  const int to = last < p0 ? from : long1 ? min(end1, last + P) : end1;
+  const bool piece0 = long0 && from < min(end0, p1);  // the first is a piece,
+  const bool piece1 = long1 && k1 != k0;              // or the last
+  const int slot0 = from == begin0;                   // an id's first piece has a place of its own
+  if (lane == 0) A.tail[chunk] = piece0 && slot0 ? k0 : piece1 ? k1 : -1;
+  if (from == to) return;
+  const int q0 = from - p0, q1 = to - p0;  // at most two chunks' length, less one
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  bool head = piece0;
+  typedef Vec<GT, 8> Raw;
+  auto fetch = [&](int q, Raw (&v)[8]) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      if (q + u >= len) break;
-      const int k0 = __builtin_amdgcn_readlane(key, q + u);
+      const int64_t row = token_at(min(q + u, q1 - 1));
+      const GT *const p = static_cast<const GT *>(A.src) + row * A.lds + col;
+      if (cnt >= 8) {
+        v[u] = load_vec<GT, 8>(p);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += v[u][k];
-      const bool end = q + u + 1 == len;
-      if (end || __builtin_amdgcn_readlane(key, min(q + u + 1, 63)) != k0) {
+        for (int k = 0; k < 8; ++k) v[u].v[k] = k < cnt ? p[k] : (GT)0.f;
+      }
+    }
+  };
+  auto add = [&](int q, const Raw (&v)[8]) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (q + u >= q1) break;
+      const int id = key_at(q + u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] += float(v[u].v[k]);
+      const bool end = q + u + 1 == q1;
+      if (end || key_at(q + u + 1) != id) {
         if (cnt > 0) {
-          if (head || (end && after))
-            store8(A.part + (2 * chunk + (head ? 0 : 1)) * A.cpad + col, cnt, s);
+          if (head || (end && piece1))
+            store8(A.part + (2 * chunk + (head ? slot0 : 1)) * A.cpad + col, cnt, s);
           else
-            put_row<DT>(A, k0, col, cnt, s);
+            put_row<DT>(A, id, col, cnt, s);
         }
         head = false;
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] = 0.f;
       }
     }
+  };
+  // eight rows are added while the next eight load
+  Raw r0[8], r1[8];
+  fetch(q0, r0);
+  for (int q = q0; q < q1; q += 16) {
+    if (q + 8 < q1) fetch(q + 8, r1);
+    add(q, r0);
+    if (q + 16 < q1) fetch(q + 16, r0);
+    if (q + 8 < q1) add(q + 8, r1);
   }
 }
 
-// the ids that cross the end of chunk blockIdx.x and began in it: 64 vectors of columns a
-// workgroup, the parts dealt to sixteen wavefronts in runs, which are then added in order
+// The ids in pieces: a wavefront looks at a chunk, 512 columns, and adds up the pieces of the id that
+// began there if they are few.  Many are dealt to the workgroup's eight wavefronts in runs, whose
+// sums are then added in order.  Piece i begins in the i-th chunk after the id's first.
+constexpr int JOIN = 8, FEW = 16;
+
 template <typename DT>
-__global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs A) {
-  __shared__ float red[16][8][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int total = A.start[A.vocab];
-  const int64_t chunk = blockIdx.x, end = (chunk + 1) * A.chunk;
-  if (end >= total) return;
-  const int key = A.key[end - 1];
-  if (A.key[end] != key || A.start[key] < chunk * A.chunk) return;
-  const int64_t last = (A.start[key + 1] - 1) / A.chunk;  // the chunk that holds its last token
-  const int n = int(last - chunk) + 1;                    // parts: this chunk's tail, the others' heads
+__global__ __launch_bounds__(64 * JOIN) void k_embed_join(EmbedArgs A) {
+  __shared__ float red[JOIN][8][64];
+  __shared__ int ids[JOIN], pieces[JOIN];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = blockIdx.y * 512 + lane * 8, cnt = min(8, A.c - col);
-  const int per = (n + 15) / 16, a = min(wave * per, n), b = min(a + per, n);
-  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (cnt > 0) {
-#pragma unroll 4
+  auto sum = [&](int64_t chunk, int a, int b, float (&s)[8]) {
+    if (cnt <= 0) return;
+#pragma unroll 8
     for (int i = a; i < b; ++i) {
       float v[8];
       load8(A.part + (2 * (chunk + i) + (i ? 0 : 1)) * A.cpad + col, cnt, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) s[k] += v[k];
     }
+  };
+  const int64_t mine = blockIdx.x * int64_t(JOIN) + wave;
+  const int key = mine < A.chunks ? A.tail[mine] : -1;
+  int n = 0;
+  if (key >= 0) {
+    n = (A.start[key + 1] - A.start[key] + A.chunk - 1) / A.chunk;
+    if (n <= FEW) {
+      float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      sum(mine, 0, n, s);
+      if (cnt > 0) put_row<DT>(A, key, col, cnt, s);
+      n = 0;
+    }
   }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) red[wave][k][lane] = s[k];
+  if (lane == 0) {
+    ids[wave] = key;
+    pieces[wave] = n;
+  }
   __syncthreads();
-  if (wave == 0 && cnt > 0) {
-    const int waves = (n + per - 1) / per;
-    for (int w = 1; w < waves; ++w)
+  for (int w = 0; w < JOIN; ++w) {
+    const int m = pieces[w];
+    if (!m) continue;
+    const int per = (m + JOIN - 1) / JOIN, a = min(wave * per, m), b = min(a + per, m);
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    sum(blockIdx.x * int64_t(JOIN) + w, a, b, s);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += red[w][k][lane];
-    put_row<DT>(A, key, col, cnt, s);
+    for (int k = 0; k < 8; ++k) red[wave][k][lane] = s[k];
+    __syncthreads();
+    if (wave == 0 && cnt > 0) {
+      const int waves = (m + per - 1) / per;
+      for (int q = 1; q < waves; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += red[q][k][lane];
+      put_row<DT>(A, ids[w], col, cnt, s);
+    }
+    __syncthreads();
   }
 }
 
@@ -285,13 +401,20 @@ void forward(hipStream_t s, const EmbedArgs &a) {
 
 template <typename GT, typename DT>
 void backward(hipStream_t s, const EmbedArgs &a) {
-  const int tiles = (a.c + 511) / 512;
-  const int sums = int((int64_t(a.chunks) * tiles + 3) / 4);
-  const int64_t rows = (a.vocab + 3) / 4;
-  const int zeros = a.accumulate ? 0 : int(rows < 2048 ? rows : 2048);
-  hipLaunchKernelGGL((k_embed_sum<GT, DT>), dim3(uint32_t(sums + zeros)), dim3(256), 0, s, a, tiles, sums);
-  if (a.chunks > 1)
-    hipLaunchKernelGGL(k_embed_join<DT>, dim3(uint32_t(a.chunks - 1), uint32_t(tiles)), dim3(1024), 0, s, a);
+  // a range for each compute unit, as far as the counts fit
+  const int64_t even = (a.vocab + 255) / 256;
+  const int range = int(even < MAX_RANGE ? even : MAX_RANGE);
+  const dim3 ranges(uint32_t((a.vocab + range - 1) / range));
+  if (a.ids64)
+    hipLaunchKernelGGL(k_embed_sort<true>, ranges, dim3(64 * SECTIONS), 0, s, a, range);
+  else
+    hipLaunchKernelGGL(k_embed_sort<false>, ranges, dim3(64 * SECTIONS), 0, s, a, range);
+  const int tiles = (a.c + 511) / 512, zeros = a.accumulate ? 0 : int((a.vocab + 255) / 256);
+  hipLaunchKernelGGL((k_embed_sum<GT, DT>), dim3(uint32_t(zeros + (int64_t(a.chunks) * tiles + 3) / 4)), dim3(256), 0, s,
+                     a, tiles, zeros);
+  if (a.tokens > a.chunk)
+    hipLaunchKernelGGL(k_embed_join<DT>, dim3(uint32_t((a.chunks + JOIN - 1) / JOIN), uint32_t(tiles)), dim3(64 * JOIN),
+                       0, s, a);
 }
 
 uint64_t align16(uint64_t v) { return (v + 15) & ~uint64_t(15); }
@@ -307,7 +430,10 @@ void embed_forward(hipStream_t s, const EmbedArgs &a, int wtype, int ytype) {
 }
 
 uint64_t embed_plan(EmbedArgs &a, char *ws) {
+  // positions a wavefront begins with: 16 wavefronts for each compute unit, if there are as many
+  const int64_t tiles = (a.c + 511) / 512;
   a.chunk = 64;
+  while (a.chunk > 16 && (a.tokens + a.chunk - 1) / a.chunk * tiles < 4096) a.chunk /= 2;
   a.chunks = int((a.tokens + a.chunk - 1) / a.chunk);
   a.cpad = (a.c + 7) / 8 * 8;
   uint64_t at = 0;
@@ -317,21 +443,18 @@ uint64_t embed_plan(EmbedArgs &a, char *ws) {
     return p;
   };
   const uint64_t start = take(4 * uint64_t(a.vocab + 1)), perm = take(4 * uint64_t(a.tokens)),
-                 key = take(4 * uint64_t(a.tokens)), part = take(8 * uint64_t(a.chunks) * a.cpad);
+                 key = take(4 * uint64_t(a.tokens)), tail = take(4 * uint64_t(a.chunks)), part = take(8 * uint64_t(a.chunks) * a.cpad);
   if (ws) {
     a.start = reinterpret_cast<int *>(ws + start);
     a.perm = reinterpret_cast<int *>(ws + perm);
     a.key = reinterpret_cast<int *>(ws + key);
+    a.tail = reinterpret_cast<int *>(ws + tail);
     a.part = reinterpret_cast<float *>(ws + part);
   }
   return at;
 }
 
 void embed_backward(hipStream_t s, const EmbedArgs &a, int gtype, int dtype) {
-  // a range for each compute unit, as far as the counts fit
-  const int64_t even = (a.vocab + 255) / 256;
-  const int range = int(even < MAX_RANGE ? even : MAX_RANGE);
-  hipLaunchKernelGGL(k_embed_sort, dim3(uint32_t((a.vocab + range - 1) / range)), dim3(64 * SECTIONS), 0, s, a, range);
   if (gtype == SEQ_F32)
     dtype == SEQ_F32 ? backward<float, float>(s, a) : backward<float, __bf16>(s, a);
   else

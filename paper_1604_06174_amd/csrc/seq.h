@@ -48,7 +48,8 @@ struct EmbedArgs {
   int *start;   // [vocab + 1] first sorted position of each id
   int *perm;    // [tokens] token at each sorted position
   int *key;     // [tokens] its id
-  float *part;  // [2 chunks][cpad] sums of ids that cross a chunk's ends
+  int *tail;    // [chunks] the id in pieces that begins in a chunk, or -1
+  float *part;  // [2 chunks][cpad] sums of the pieces that begin in a chunk: a later piece, a first one
   int chunk, chunks, cpad;
 };
 

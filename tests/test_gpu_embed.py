@@ -1,8 +1,9 @@
 """GPU parity of the embedding and its gradient (op_embed_*) with the float64 oracle.
 
-Bars: half a step of the output's type, plus for a gradient L 2^-24 times the sum of
-magnitudes: an id's rows are added in chunks of at most 64, at most 64 chunks' parts
-in a wavefront at the counts here, and sixteen wavefronts: below 256 operations in a chain.
+Bars: half a step of the output's type, plus for a gradient the chain of sums that a row
+of n tokens of one id may pass, 2^-24 of the sum of magnitudes each: at most 64 in a wavefront,
+then ceil(n / 16) pieces at most, dealt to eight wavefronts if there are more than 16, the
+eight sums, and three more for the scale, the addition and the store.
 """
 import numpy as np
 import pytest
@@ -13,7 +14,11 @@ from seq_cases import DEV, STEP, K, Rows, close, code, host, rounded
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-L = 256 * 2.0 ** -24
+
+def chain(ids):
+    n = int(np.bincount(ids[ids >= 0]).max()) if (ids >= 0).any() else 1
+    pieces = -(-n // 16)
+    return (64 + (pieces if pieces <= 16 else -(-pieces // 8)) + 8 + 3) * 2.0 ** -24
 
 
 def device_ids(ids, wide):
@@ -50,12 +55,13 @@ def check(ids, g, vocab, scale=1.0, gt="f32", dt="f32", accumulate=None, **kw):
     want, mag = S.embed_backward(np.asarray(ids), g, vocab, scale)
     if accumulate is not None:
         want, mag = want + accumulate, mag + np.abs(accumulate)
-    close("dw", got, want, STEP[dt] * np.abs(want) + L * mag)
+    close("dw", got, want, STEP[dt] * np.abs(want) + chain(np.asarray(ids)[np.asarray(ids) < vocab]) * mag)
 
 
 @pytest.mark.parametrize("tokens,vocab,c", [(1, 1, 1), (1, 50, 7), (7, 3, 9), (64, 5, 8), (65, 2, 520), (1000, 40, 333),
                                             (4099, 97, 64), (5000, 30011, 40), (300, 300000, 16), (20011, 1030, 1030),
-                                            (60000, 2, 8), (60000, 1, 24)])
+                                            (60000, 2, 8), (60000, 1, 24), (64, 1, 8), (65, 1, 8), (129, 2, 600), (640, 10, 9),
+                                            (6400, 100, 17)])
 def test_gradient_sizes(tokens, vocab, c):
     rng = np.random.default_rng(tokens + vocab)
     check(words(rng, tokens, vocab), rng.standard_normal((tokens, c)), vocab, scale=3.7)
@@ -86,23 +92,20 @@ def test_no_valid_id():
 
 
 def test_each_id_is_added_in_the_order_of_its_tokens():
-    # sums whose value depends on the order: within a chunk they are a running sum
+    # sums whose value depends on the order: of few tokens they are a running sum
     rng = np.random.default_rng(3)
     n, vocab = 600, 40
     ids = np.repeat(np.arange(40), 15)[rng.permutation(600)]
     g = (rng.standard_normal((n, 8)) * 10.0 ** rng.integers(-4, 5, (n, 1))).astype(np.float32)
     got = backward(ids, g.astype(np.float64), vocab)
-    order, p, exact = np.argsort(ids, kind="stable"), 0, 0
+    order, p = np.argsort(ids, kind="stable"), 0
     for v in range(vocab):
         rows = order[p:p + 15]
-        if p // 64 == (p + 14) // 64:
-            s = np.zeros(8, np.float32)
-            for i in rows:
-                s = s + g[i]
-            assert np.array_equal(got[v], s.astype(np.float64))
-            exact += 1
+        s = np.zeros(8, np.float32)
+        for i in rows:
+            s = s + g[i]
+        assert np.array_equal(got[v], s.astype(np.float64))
         p += 15
-    assert exact > 20
 
 
 @pytest.mark.parametrize("wt", ["f32", "bf16"])
