@@ -59,13 +59,67 @@ struct Sequence {
 
 __device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-// The sequence that tile `tile` of `size` rows lies in, `per` rows to each row of the
-// tensor that `off` counts.  Sequence s owns the tiles from off[s] per / size + s on: as many
-// as its rows can take whatever their number, so a tile's sequence is found without adding
-// lengths up.  false: the tile is past its sequence's rows.
-__device__ __forceinline__ bool find_tile(const AttnArgs &A, const int *off, int64_t total, int per, int size, int tile,
-                                          Sequence &q) {
+__device__ __forceinline__ void rows_of(const AttnArgs &A, int s, Sequence &q) {
+  q.q0 = clamp_row(A.qoff[s], 0, A.tq);
+  q.lq = int(clamp_row(A.qoff[s + 1], q.q0, A.tq) - q.q0);
+  q.k0 = clamp_row(A.koff[s], 0, A.tk);
+  q.lk = int(clamp_row(A.koff[s + 1], q.k0, A.tk) - q.k0);
+}
+
+// sum over the wavefront's lanes
+__device__ __forceinline__ int wave_add(int v) {
+  v += __float_as_int(lane_xor<1>(__int_as_float(v)));
+  v += __float_as_int(lane_xor<2>(__int_as_float(v)));
+  v += __float_as_int(lane_xor<4>(__int_as_float(v)));
+  v += __float_as_int(lane_xor<8>(__int_as_float(v)));
+  float a = __int_as_float(v), b = a;
+  swap_rows<16>(a, b);
+  v = __float_as_int(a) + __float_as_int(b);
+  a = b = __int_as_float(v);
+  swap_rows<32>(a, b);
+  return __builtin_amdgcn_readfirstlane(__float_as_int(a) + __float_as_int(b));
+}
+
+// The `index`-th tile of `size` rows, `per` rows to each token of the queries (QUERIES) or of the keys.
+// false: there is none.
+//
+// Up to 64 sequences, a lane each, are ordered by their tiles' work, longest first: a causal tile's
+// is its place in its sequence (of queries with the keys before them, of keys with the queries
+// behind them), so the tiles of a level w or above are counted, sum over the sequences of how far they
+// reach past w, and the level is searched for.  Then no long tile is left to the end, and no
+// workgroup is without one.
+// More sequences take the tiles from off[s] per / size + s on each: as many as its rows can take
+// whatever their number, so a tile's sequence is found without adding lengths up.
+template <bool QUERIES>
+__device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int size, int tiles, int index, Sequence &q) {
   const int lane = threadIdx.x & 63;
+  if (A.seqs <= 64) {
+    Sequence mine{0, 0, 0, 0, 0};
+    if (lane < A.seqs) rows_of(A, lane, mine);
+    const int n = int((int64_t(QUERIES ? mine.lq : mine.lk) * per + size - 1) / size);
+    const int low = QUERIES && A.causal ? int(int64_t(max(0, mine.lk - mine.lq)) * per / size) : 0;
+    auto above = [&](int w) { return wave_add(max(0, min(n, low + n - w))); };
+    const int total = above(0);
+    if (index >= total) return false;
+    int lo = 0, hi = 1;
+    while (above(hi) > index) lo = hi, hi *= 2;
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (above(mid) > index) lo = mid;
+      else hi = mid;
+    }
+    // the sequences with a tile at this level, in order
+    const int rank = index - above(lo + 1);
+    const bool has = lo >= low && lo < low + n;
+    const uint64_t all = __ballot(has);
+    const int who = __ffsll((unsigned long long)__ballot(has && __popcll(all & ((1ull << lane) - 1)) == rank)) - 1;
+    rows_of(A, who, q);
+    const int t = lo - __builtin_amdgcn_readlane(low, who);
+    q.first = int64_t(QUERIES ? t : __builtin_amdgcn_readlane(n, who) - 1 - t) * size;
+    return true;
+  }
+  const int *const off = QUERIES ? A.qoff : A.koff;
+  const int tile = QUERIES ? tiles - 1 - index : index;  // later queries see more, earlier keys are seen more
   int lo = 0, n = A.seqs;
   while (true) {  // 64 sequences at a time, then 64 ranges of them ...
     const int step = (n + 63) / 64, s = lo + lane * step;
@@ -77,14 +131,9 @@ __device__ __forceinline__ bool find_tile(const AttnArgs &A, const int *off, int
     if (step == 1) break;
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  const int64_t base = int64_t(off[lo]) * per / size + lo;
-  q.q0 = clamp_row(A.qoff[lo], 0, A.tq);
-  q.lq = int(clamp_row(A.qoff[lo + 1], q.q0, A.tq) - q.q0);
-  q.k0 = clamp_row(A.koff[lo], 0, A.tk);
-  q.lk = int(clamp_row(A.koff[lo + 1], q.k0, A.tk) - q.k0);
-  q.first = (tile - base) * size;
-  const int64_t rows = int64_t(off == A.qoff ? q.lq : q.lk) * per;
-  return q.first >= 0 && q.first < rows;
+  rows_of(A, lo, q);
+  q.first = (tile - (int64_t(off[lo]) * per / size + lo)) * size;
+  return q.first >= 0 && q.first < int64_t(QUERIES ? q.lq : q.lk) * per;
 }
 
 // ---- tiles in LDS ----------------------------------------------------------
@@ -98,29 +147,44 @@ __device__ __forceinline__ int swizzle(int row) {
 
 // The loader of a tile of ROWS rows, `ld` elements apart, straight into LDS: zeros for rows
 // from `valid` on and columns from `dim` on.  A thread loads the same columns of each of its
-// rows, whose order of chunks is the same (they are sixteen rows apart, or 32).
+// rows, whose order of chunks is the same (they are sixteen rows apart, or 32).  Whole tiles take
+// addresses of a scalar and the lane's own 32 bits, so they cost the vector unit nothing.
 template <int D, int ROWS, int THREADS>
 struct Loader {
   static constexpr int C = D / 8, STEP = THREADS / C, N = ROWS / STEP;
   static_assert(STEP % 16 == 0 && ROWS % STEP == 0, "rows with the same order of chunks");
-  const __bf16 *src;  // the thread's first chunk of row 0's tile
-  int64_t ld;
-  bool in;            // its columns are below dim
+  const char *src;  // row 0
+  int64_t pitch;    // bytes from row to row
+  unsigned place;   // the lane's first chunk from the tile's first row, in bytes
+  bool in, whole;   // its columns are below dim; all lanes' are, and 32 bits hold their places
 
-  __device__ __forceinline__ Loader(const __bf16 *base, int64_t ld_, int dim) : ld(ld_) {
+  __device__ __forceinline__ Loader(const __bf16 *base, int64_t ld, int dim)
+      : src(reinterpret_cast<const char *>(base)), pitch(2 * ld) {
     const int row = threadIdx.x / C, col = ((threadIdx.x % C) ^ swizzle<D>(row)) * 8;
-    src = base + row * ld + col;
+    place = unsigned(row) * unsigned(pitch) + 2 * col;
     in = col < dim;
+    whole = dim == D && pitch < (1 << 24);
   }
-  // the tile from row `first` on, `offset` elements further
+  // the tile from row `first` on, `offset` bytes further
   __device__ __forceinline__ void load(unsigned char *lds, int64_t first, int valid, int64_t offset = 0) const {
-    const __bf16 *p = src + first * ld + offset;
-    unsigned char *const to = lds + (threadIdx.x >> 6) * 1024;
+    const char *const p = src + first * pitch + offset;
+    unsigned char *const to = lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+    if (whole && valid >= ROWS) {
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const bool ok = in && int(threadIdx.x / C) + c * STEP < valid;
-      const void *const q = ok ? static_cast<const void *>(p + c * STEP * ld) : g_zeros + 4 * (threadIdx.x & 255);
-      __builtin_amdgcn_global_load_lds(q, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
+      for (int c = 0; c < N; ++c) {
+        const char *q = p + c * STEP * pitch;
+        asm("" : "+s"(q));  // the scalar sum first
+        __builtin_amdgcn_global_load_lds(q + place, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
+      }
+    } else {
+      const int row = threadIdx.x / C, col = ((threadIdx.x % C) ^ swizzle<D>(row)) * 8;
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const bool ok = in && row + c * STEP < valid;
+        const void *const q = ok ? static_cast<const void *>(p + (row + c * STEP) * pitch + 2 * col)
+                                 : g_zeros + 4 * (threadIdx.x & 255);
+        __builtin_amdgcn_global_load_lds(q, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
+      }
     }
   }
 };

@@ -42,10 +42,10 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   constexpr int BM = 128, BN = 64, SUBS = BN / 32, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int kvh = blockIdx.x % A.kv_heads, tile = tiles - 1 - int(blockIdx.x / A.kv_heads);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
   Sequence sq;
-  if (!find_tile(A, A.qoff, A.tq, A.rep, BM, tile, sq)) return;
+  if (!find_tile<true>(A, A.rep, BM, tiles, tile, sq)) return;
   const int64_t rows = int64_t(sq.lq) * A.rep;
   const int64_t row = sq.first + wave * 32 + (lane & 31);
   const bool valid = row < rows;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   const int token = int(r / A.rep), head = kvh * A.rep + int(r - int64_t(token) * A.rep);
   const int past = sq.lk - sq.lq;
   const int lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;
-  const int lim_lo = __builtin_amdgcn_readfirstlane(lim), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+  const int lim_lo = __builtin_amdgcn_readfirstlane(lim);
   const int64_t last = min(sq.first + BM, rows) - 1;
   const int kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
   const int end = (kend + BN - 1) / BN;
@@ -105,13 +105,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
     }
   };
   if (end > 0) load(0, kt0, vt0);
-  two_kinds(end, min(end, lim_lo / BN), [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+  const int full = min(end, lim_lo / BN) & ~1;  // tiles that every row of the wavefront sees whole
+  two_kinds(end, full, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
     if (it + 1 < end) load(it + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(it, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
   if (__any(bad != 0))
-    add_special<D>(dq, kp, A.ldk, A.dim, lim_lo / BN * BN, lim_hi, true, [&](int j) { return j < lim; });
+    add_special<D>(dq, kp, A.ldk, A.dim, full * BN, min(end * BN, sq.lk), true, [&](int j) { return j < lim; });
   if (valid) store_row<D>(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
 }
 
@@ -126,16 +127,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   __shared__ __align__(16) unsigned char qt0[BN * D * 2], qt1[BN * D * 2], gt0[BN * D * 2], gt1[BN * D * 2];
   __shared__ __align__(16) unsigned char vt[BM * D * 2];
   __shared__ __align__(16) float st0[128], st1[128];  // lse in base 2 | delta, 64 places each
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
   Sequence sq;
-  if (!find_tile(A, A.koff, A.tk, 1, BM, tile, sq)) return;
+  if (!find_tile<false>(A, 1, BM, 0, tile, sq)) return;
   const int first = int(sq.first), key = first + wave * 32 + (lane & 31);
   const bool valid = key < sq.lk;
   const int past = sq.lk - sq.lq;
-  // the first query that sees the key, the wavefront's and the workgroup's first
+  // the first query that sees the key, and the workgroup's first tile
   const int from = A.causal ? max(0, key - past) : 0;
-  const int from_lo = __builtin_amdgcn_readfirstlane(from), from_hi = __builtin_amdgcn_readlane(from, 31);
   const int begin = (A.causal ? max(0, first - past) : 0) / BN, end = (sq.lq + BN - 1) / BN;
   const int heads = A.rep / A.parts, head0 = kvh * A.rep + int(blockIdx.y) * heads;
   const int per = max(0, end - begin), n = per * heads;  // tiles of a head, of all
@@ -152,8 +152,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
       gload(A.g + sq.q0 * A.ldo + head0 * A.hso, A.ldo, A.dim);
   auto load = [&](int h, int t, unsigned char *qt, unsigned char *gt, float *st) __attribute__((always_inline)) {
     const int t0 = t * BN;
-    qload.load(qt, t0, sq.lq - t0, h * A.hsq);
-    gload.load(gt, t0, sq.lq - t0, h * A.hso);
+    qload.load(qt, t0, sq.lq - t0, 2 * h * A.hsq);
+    gload.load(gt, t0, sq.lq - t0, 2 * h * A.hso);
     // a wavefront each; rows past the sequence's: p = exp2(-inf)
     if (wave < 2) {
       const bool ok = t0 + lane < sq.lq && lane < BN;
@@ -227,7 +227,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
     Loader<D, BM, 256>(A.v + sq.k0 * A.ldv + kvh * A.hsv, A.ldv, A.dim).load(vt, first, sq.lk - first);
     next(qt0, gt0, st0);
   }
-  two_kinds(n, (end - seen) * heads, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
+  const int whole = (end - seen) * heads;  // tiles that see all of the workgroup's keys
+  two_kinds(n, whole & ~1, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
     if (it + 1 < n) next(place ? qt0 : qt1, place ? gt0 : gt1, place ? st0 : st1);
     work(now.t * BN, place ? qt1 : qt0, place ? gt1 : gt0, place ? st1 : st0, masked);
@@ -236,7 +237,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   if (__any((badq | badg) != 0))
     for (int h = 0; h < heads; ++h) {
       auto sees = [&](int r) { return r >= from; };
-      const int row1 = min(sq.lq, (from_hi + BN - 1) / BN * BN), row0 = min(row1, from_lo / BN * BN);
+      // the tiles with tests: an odd one of the others, which comes just before them, is taken so too
+      const int row0 = begin * BN, row1 = min(sq.lq, (seen + (h == heads - 1 && (whole & 1))) * BN);
       add_special<D>(dv, A.g + sq.q0 * A.ldo + (head0 + h) * A.hso, A.ldo, A.dim, row0, row1, false, sees);
       add_special<D>(dk, A.q + sq.q0 * A.ldq + (head0 + h) * A.hsq, A.ldq, A.dim, row0, row1, true, sees);
     }

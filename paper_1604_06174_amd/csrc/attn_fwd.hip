@@ -4,10 +4,7 @@
 // The query rows that share a key head, (token, head of the group) in this order, are one
 // matrix: a key tile is read once for all of them, and single tokens fill tiles as far as
 // their heads go.  Each of a workgroup's wavefronts keeps 32 of these rows; the keys come by in
-// tiles through LDS, the next one loading while one is worked on.
-//   many rows (k_attn_fwd<D, 4>): four wavefronts with 32 rows each share tiles of 64 keys
-//   few rows (k_attn_fwd<D, 1>): four wavefronts with the same 32 rows take a quarter each of tiles
-//     of 128 keys and join their sums at the end
+// tiles through LDS, later ones loading while one is worked on (k_attn_many, k_attn_few).
 // Where there are too few workgroups for the chip, the keys are split over several, whose
 // unfinished rows go to the workspace and are joined by k_attn_join.
 #include "attn.h"
@@ -18,102 +15,283 @@ namespace {
 
 using namespace at;
 
-template <int D, int WQ>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
-  constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = WQ == 4 ? 64 : 128, SUBS = BN / 32 / WK, T = D / 32, KK = D / 16;
-  __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wq = WQ == 4 ? wave : 0, wk = WQ == 4 ? 0 : wave;
-  const int kvh = blockIdx.x % A.kv_heads, tile = tiles - 1 - int(blockIdx.x / A.kv_heads);
-  Sequence sq;
-  if (!find_tile(A, A.qoff, A.tq, A.rep, BM, tile, sq)) return;
-  const int64_t rows = int64_t(sq.lq) * A.rep;
+// A row's softmax as it goes on: exponentials are powers of two relative to `base`, and l is their
+// sum.  The base is a whole number, so that moving it scales by a power of two, which rounds
+// nothing; it is moved only when an exponential would exceed 2^8, which keeps the sums far inside
+// fp32.
+struct Sums {
+  float sc;  // of scores to exponents
+  float base = -INFINITY, l = 0.f, top = 0.f;
 
-  // the lane's query
-  const int64_t row = sq.first + wq * 32 + (lane & 31);
-  const bool valid = row < rows;
-  const int64_t r = valid ? row : rows - 1;
-  const int token = int(r / A.rep), head = kvh * A.rep + int(r - int64_t(token) * A.rep);
-  const int past = sq.lk - sq.lq;
-  const int lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;  // keys it sees
-  const int lim_lo = __builtin_amdgcn_readfirstlane(lim), lim_hi = __builtin_amdgcn_readlane(lim, 31);  // the wavefront's least and most
-  const int64_t last = min(sq.first + BM, rows) - 1;
-  const int kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
-  const int all = (kend + BN - 1) / BN;
-  const int begin = int(int64_t(all) * blockIdx.y / gridDim.y), end = int(int64_t(all) * (blockIdx.y + 1) / gridDim.y);
+  __device__ __forceinline__ explicit Sums(float scale) : sc(scale) {}
+  // does a row of the wavefront have to move its base for scores up to `score`?
+  __device__ __forceinline__ bool rises(float score) {
+    top = score * sc;
+    return __any(top - base > 8.f);
+  }
+  // moves it, and says what the sums so far are to be scaled by
+  __device__ __forceinline__ float move() {
+    const float to = fmaxf(base, ceilf(top));
+    const float f = to == base ? 1.f : exp2_fast(base - to);
+    base = to;
+    l *= f;
+    return f;
+  }
+  __device__ __forceinline__ float exponential(float score) const {
+    return exp2_fast(fmaf(score, sc, base == -INFINITY ? 0.f : -base));
+  }
+};
+
+// A workgroup's rows and the keys they see: what a lane needs of its query.
+template <int BM>
+struct Query {
+  Sequence sq;
+  int64_t rows;
+  int token, head, lim;  // lim: keys it sees
+  int lim_lo;            // the wavefront's least
+  int kend;              // the workgroup's most
+  bool valid;
+
+  // the lane's row is `row` of the tile; false: the tile has none
+  __device__ __forceinline__ bool find(const AttnArgs &A, int tiles, int tile, int kvh, int row) {
+    if (!find_tile<true>(A, A.rep, BM, tiles, tile, sq)) return false;
+    rows = int64_t(sq.lq) * A.rep;
+    valid = sq.first + row < rows;
+    const int64_t r = valid ? sq.first + row : rows - 1;
+    token = int(r / A.rep);
+    head = kvh * A.rep + int(r - int64_t(token) * A.rep);
+    const int past = sq.lk - sq.lq;
+    lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;
+    lim_lo = __builtin_amdgcn_readfirstlane(lim);
+    const int64_t last = min(sq.first + BM, rows) - 1;
+    kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
+    return true;
+  }
+};
+
+// o (unscaled) and the sums of a lane's row to their places: o / l and lse, or the parts of a split
+template <int D>
+__device__ __forceinline__ void finish(const AttnArgs &A, int head, int64_t token, const f32x16 (&o)[D / 32], float base,
+                                       float l) {
+  const int64_t at_row = head * A.tq + token;
+  const bool first = (threadIdx.x & 63) < 32;
+  if (gridDim.y > 1) {
+    const int64_t p = int64_t(blockIdx.y) * A.heads * A.tq + at_row;
+    if (first) {
+      A.pml[2 * p] = base;
+      A.pml[2 * p + 1] = l;
+    }
+    store_part<D>(A.po + p * A.dim, o, 1.f, A.dim);
+    return;
+  }
+  if (first) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
+  store_row<D>(A.o + token * A.ldo + head * A.hso, o, l == 0.f ? 0.f : 1.f / l, A.dim);
+}
+
+// the split's share of n tiles
+__device__ __forceinline__ void share(int n, int &begin, int &end) {
+  begin = int(int64_t(n) * blockIdx.y / gridDim.y);
+  end = int(int64_t(n) * (blockIdx.y + 1) / gridDim.y);
+}
+
+// Four wavefronts of 32 rows.  The keys come by 32 at a time, two to a tile, in three stages that are in the
+// registers together: the scores of the next 32, the exponentials of these, and the product with the
+// values of the last.  The three need nothing of each other, so matrix and vector units work
+// side by side; one stage after the other, a compute unit's two workgroups keep either idle
+// half of the time (16384 tokens, 16/4 heads of 128: TIME_OLD us one after the other, TIME_NEW us so).
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attn_many(AttnArgs A, int tiles) {
+  constexpr int BM = 128, BN = 64, T = D / 32, KK = D / 16;
+  __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
+  Query<BM> y;
+  if (!y.find(A, tiles, tile, kvh, wave * 32 + (lane & 31))) return;
+  const int lk = y.sq.lk;
+  int begin, end;
+  share((y.kend + BN - 1) / BN, begin, end);
+  const int n = end - begin;
+  y.lim = min(y.lim, end * BN);  // the scores that follow the split's last keys are nobody's
 
   bf16x8 q[KK];
   {
-    const __bf16 *p = A.q + (sq.q0 + token) * A.ldq + head * A.hsq;
+    const __bf16 *p = A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
   }
   const Places<D> places;
-  const __bf16 *const vp = A.v + sq.k0 * A.ldv + kvh * A.hsv;
-  const Loader<D, BN, 256> kload(A.k + sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
+  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
+  auto load_k = [&](int it, unsigned char *kt) __attribute__((always_inline)) {
+    kload.load(kt, int64_t(it) * BN, lk - it * BN);
+  };
+  auto load_v = [&](int it, unsigned char *vt) __attribute__((always_inline)) {
+    vload.load(vt, int64_t(it) * BN, lk - it * BN);
+  };
+
+  f32x16 o[T], s;    // s: the scores of the keys whose turn it is
+  bf16x8 p[2];       // probabilities of the last 32, not yet in o
+  clear(o);
+  Sums z(A.scale * LOG2E);
+  unsigned bad = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[0][e] = p[1][e] = (__bf16)0.f;
+
+  // s holds the scores of the 32 keys from j on: those that the row does not see become -inf, and
+  // the base is moved if it would let an exponential exceed 2^8 (most tiles leave it)
+  auto meet = [&](int j, auto masked) __attribute__((always_inline)) {
+    const int left = y.lim - j - 4 * (lane >> 5);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (decltype(masked)::value && 8 * (i / 4) + i % 4 >= left) s[i] = -INFINITY;
+      top = fmaxf(top, s[i]);
+    }
+    if (!z.rises(halves_max(top))) return;
+    const float f = z.move();
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(float(p[c][e]) * f);  // a power of two: exact
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] *= f;
+  };
+  // o += p v, the values of 32 rows of a tile
+  auto product = [&](const Places<D> &at, const unsigned char *vt, int first, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      if constexpr (decltype(masked)::value) add_rows_finite<D>(o, at, vt, first + 16 * c, p[c], bad);
+      else add_rows<D>(o, at, vt, first + 16 * c, p[c]);
+    }
+  };
+  // one turn: scores of the 32 rows of `kt` from kfirst on (the keys from j on), exponentials of s,
+  // the product of p with the rows of `vt` from vfirst on
+  auto turn = [&](int j, const unsigned char *kt, int kfirst, const unsigned char *vt, int vfirst, auto masked)
+      __attribute__((always_inline)) {
+    const Places<D> at = places.here();
+    f32x16 next[1];
+    clear(next);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) next[0] = mfma(at.rows(kt, kfirst, kk), q[kk], next[0]);
+    product(at, vt, vfirst, masked);
+    float l0 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = z.exponential(s[i]);
+      l0 += s[i];
+    }
+    z.l += l0;
+    p[0] = operand(s, 0);
+    p[1] = operand(s, 1);
+    s = next[0];
+  };
+
+  if (n > 0) {
+    load_k(begin, kt0);
+    // what p multiplies before there are values
+    for (int e = threadIdx.x; e < BN * D * 2 / 16; e += 256) reinterpret_cast<u32x4 *>(vt1)[e] = u32x4{0u, 0u, 0u, 0u};
+    tile_barrier();
+    load_v(begin, vt0);
+    if (n > 1) load_k(begin + 1, kt1);
+    const Places<D> at = places.here();
+    clear(*reinterpret_cast<f32x16(*)[1]>(&s));
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) s = mfma(at.rows(kt0, 0, kk), q[kk], s);
+    meet(begin * BN, std::true_type());
+  }
+  // Tiles which every row of the wavefront sees whole, and the next one too, are met without tests.
+  const int full = max(0, min(n, y.lim_lo / BN - begin) - 1) & ~1;
+  two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
+    const int it = begin + i;
+    unsigned char *const kt = place ? kt1 : kt0, *const kn = place ? kt0 : kt1, *const vt = place ? vt1 : vt0,
+                        *const vn = place ? vt0 : vt1;
+    // the tile's second scores; the values of the last tile's second half
+    turn(it * BN + 32, kt, 32, vn, 32, masked);
+    meet(it * BN + 32, masked);
+    tile_barrier();  // this tile's values and the next one's keys are there; their predecessors may go
+    if (i + 2 < n) load_k(it + 2, kt);
+    if (i + 1 < n) load_v(it + 1, vn);
+    turn(it * BN + 64, kn, 0, vt, 0, masked);
+    meet(it * BN + 64, masked);
+  });
+  if (n > 0) product(places.here(), (n - 1) & 1 ? vt1 : vt0, 32, std::true_type());
+  // clamped were the values from the second half of the last tile met without tests on
+  if (__any(bad != 0))
+    add_special<D>(o, vp, A.ldv, A.dim, (begin + full) * BN - (full ? 32 : 0), min(end * BN, lk), false,
+                   [&](int j) { return j < y.lim; });
+  if (y.valid) finish<D>(A, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
+}
+
+// Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
+// joined at the end.
+template <int D>
+__global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
+  constexpr int BM = 32, BN = 128, T = D / 32, KK = D / 16;
+  __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
+  Query<BM> y;
+  if (!y.find(A, tiles, tile, kvh, lane & 31)) return;
+  const int lk = y.sq.lk;
+  int begin, end;
+  share((y.kend + BN - 1) / BN, begin, end);
+  const int n = end - begin;
+
+  bf16x8 q[KK];
+  {
+    const __bf16 *p = A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
+  }
+  const Places<D> places;
+  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
 
   f32x16 o[T];
   clear(o);
-  float m = -INFINITY, l = 0.f;
-  const float sc = A.scale * LOG2E;
+  Sums z(A.scale * LOG2E);
   unsigned bad = 0;
 
   auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const Places<D> at = places.here();
-    // keys the lane's query sees from its half's first on
-    const int left = lim - (it * BN + wk * SUBS * 32) - 4 * (lane >> 5);
-    f32x16 s[SUBS];
+    const int left = y.lim - (it * BN + wave * 32) - 4 * (lane >> 5);  // keys the row sees from its half's first on
+    f32x16 s[1];
     clear(s);
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u) s[u] = mfma(at.rows(kt, (wk * SUBS + u) * 32, kk), q[kk], s[u]);
+    for (int kk = 0; kk < KK; ++kk) s[0] = mfma(at.rows(kt, wave * 32, kk), q[kk], s[0]);
     float top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (MASKED && u * 32 + 8 * (i / 4) + i % 4 >= left) s[u][i] = -INFINITY;
-        top = fmaxf(top, s[u][i]);
-      }
-    top = halves_max(top);
-    // The maximum is moved when it would let an exponential exceed 2^8: o and l stay far
-    // inside fp32, and most tiles leave them as they are.
-    if (__any((top - m) * sc > 8.f)) {
-      top = fmaxf(m, top);
-      const float f = exp2_fast((m - (top == -INFINITY ? 0.f : top)) * sc);
-      m = top;
-      l *= f;
+    for (int i = 0; i < 16; ++i) {
+      if (MASKED && 8 * (i / 4) + i % 4 >= left) s[0][i] = -INFINITY;
+      top = fmaxf(top, s[0][i]);
+    }
+    if (z.rises(halves_max(top))) {
+      const float f = z.move();
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= f;
     }
-    const float base = (m == -INFINITY ? 0.f : m) * sc;
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u)
+    for (int i = 0; i < 16; ++i) {
+      s[0][i] = z.exponential(s[0][i]);
+      z.l += s[0][i];
+    }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[u][i] = exp2_fast(fmaf(s[u][i], sc, -base));
-        l += s[u][i];
-      }
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int first = (wk * SUBS + u) * 32 + c * 16;
-        if constexpr (MASKED) add_rows_finite<D>(o, at, vt, first, operand(s[u], c), bad);
-        else add_rows<D>(o, at, vt, first, operand(s[u], c));
-      }
+    for (int c = 0; c < 2; ++c) {
+      if constexpr (MASKED) add_rows_finite<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c), bad);
+      else add_rows<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c));
+    }
   };
-  const int n = end - begin;
-  // tiles whose keys every row of the wavefront sees
-  const int whole = lim_lo - (wk + 1) * SUBS * 32 + BN;
-  const int full = max(0, min(n, (whole > 0 ? whole / BN : 0) - begin));
+  // tiles whose keys (the wavefront's quarter) every row sees
+  const int whole = y.lim_lo - (wave + 1) * 32 + BN;
+  const int full = max(0, min(n, (whole > 0 ? whole / BN : 0) - begin)) & ~1;
   auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
-    kload.load(kt, int64_t(it) * BN, sq.lk - it * BN);
-    vload.load(vt, int64_t(it) * BN, sq.lk - it * BN);
+    kload.load(kt, int64_t(it) * BN, lk - it * BN);
+    vload.load(vt, int64_t(it) * BN, lk - it * BN);
   };
   if (n > 0) load(begin, kt0, vt0);
   two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
@@ -122,61 +300,44 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs A, int tiles) {
     work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
   if (__any(bad != 0))
-    for (int it = begin; it < end; ++it) {
-      const int j0 = it * BN + wk * SUBS * 32;
-      if (j0 + SUBS * 32 > lim_lo && j0 < lim_hi)
-        add_special<D>(o, vp, A.ldv, A.dim, j0, min(j0 + SUBS * 32, sq.lk), false, [&](int j) { return j < lim; });
-    }
-  l = halves_add(l);
+    for (int it = begin + full; it < end; ++it)
+      add_special<D>(o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
+                     [&](int j) { return j < y.lim; });
 
-  if constexpr (WK > 1) {
-    // the wavefronts' sums by their common maximum, one wavefront's o (fp32, [D][32]) in each
-    // half of two of the tiles
-    __shared__ float ms[WK][32], ls[WK][32];
-    tile_barrier();
-    float *const mine = reinterpret_cast<float *>(wave < 2 ? kt0 : vt0) + (wave & 1) * D * 32;
+  // the wavefronts' sums by their largest base, one wavefront's o (fp32, [D][32]) in each
+  // half of two of the tiles
+  __shared__ float bases[4][32], ls[4][32];
+  tile_barrier();
+  float *const mine = reinterpret_cast<float *>(wave < 2 ? kt0 : vt0) + (wave & 1) * D * 32;
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+  for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mine[(32 * t + d_row(i)) * 32 + (lane & 31)] = o[t][i];
-    if (lane < 32) {
-      ms[wave][lane] = m;
-      ls[wave][lane] = l;
-    }
-    __syncthreads();
-    const float m0 = fmaxf(fmaxf(ms[0][lane & 31], ms[1][lane & 31]), fmaxf(ms[2][lane & 31], ms[3][lane & 31]));
-    float f[WK];
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < WK; ++w) {
-      f[w] = exp2_fast((ms[w][lane & 31] - (m0 == -INFINITY ? 0.f : m0)) * sc);
-      l += ls[w][lane & 31] * f[w];
-    }
-    m = m0;
-    if (wave) return;
-#pragma unroll
-    for (int t = 0; t < T; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int e = (32 * t + d_row(i)) * 32 + (lane & 31);
-        const float *const a = reinterpret_cast<const float *>(kt0) + e, *const b = reinterpret_cast<const float *>(vt0) + e;
-        // a wavefront without keys has a factor of 0 and nothing but zeros
-        o[t][i] = a[0] * f[0] + a[D * 32] * f[1] + b[0] * f[2] + b[D * 32] * f[3];
-      }
+    for (int i = 0; i < 16; ++i) mine[(32 * t + d_row(i)) * 32 + (lane & 31)] = o[t][i];
+  const float l = halves_add(z.l);
+  if (lane < 32) {
+    bases[wave][lane] = z.base;
+    ls[wave][lane] = l;
   }
-  if (!valid) return;
-  const int64_t at_row = head * A.tq + sq.q0 + token;
-  if (gridDim.y > 1) {
-    const int64_t p = int64_t(blockIdx.y) * A.heads * A.tq + at_row;
-    if (lane < 32) {
-      A.pml[2 * p] = m;
-      A.pml[2 * p + 1] = l;
-    }
-    store_part<D>(A.po + p * A.dim, o, 1.f, A.dim);
-    return;
+  __syncthreads();
+  if (wave) return;
+  float base = bases[0][lane & 31], sum = 0.f, f[4];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) base = fmaxf(base, bases[w][lane & 31]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
+    sum += ls[w][lane & 31] * f[w];
   }
-  if (lane < 32) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(m, A.scale, logf(l));
-  store_row<D>(A.o + (sq.q0 + token) * A.ldo + head * A.hso, o, l == 0.f ? 0.f : 1.f / l, A.dim);
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int e = (32 * t + d_row(i)) * 32 + (lane & 31);
+      const float *const a = reinterpret_cast<const float *>(kt0) + e, *const b = reinterpret_cast<const float *>(vt0) + e;
+      // a wavefront without keys has a factor of 0 and nothing but zeros
+      o[t][i] = a[0] * f[0] + a[D * 32] * f[1] + b[0] * f[2] + b[D * 32] * f[3];
+    }
+  if (y.valid) finish<D>(A, y.head, y.sq.q0 + y.token, o, base, sum);
 }
 
 // a row's splits joined: sixteen lanes a row, eight columns each
@@ -187,15 +348,14 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   const int head = int(at / A.tq), col = (threadIdx.x & 15) * 8;
   // rows of no sequence have no splits either
   if (token < A.qoff[0] || token >= A.qoff[A.seqs]) return;
-  const float sc = A.scale * LOG2E;
-  float m = -INFINITY;
-  for (int z = 0; z < A.splits; ++z) m = fmaxf(m, A.pml[2 * (z * n + at)]);
-  const float base = m == -INFINITY ? 0.f : m;
+  float top = -INFINITY;
+  for (int z = 0; z < A.splits; ++z) top = fmaxf(top, A.pml[2 * (z * n + at)]);
+  const float base = top == -INFINITY ? 0.f : top;
   float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 2
   for (int z = 0; z < A.splits; ++z) {
     const float lz = A.pml[2 * (z * n + at) + 1];
-    const float f = exp2_fast((A.pml[2 * (z * n + at)] - base) * sc);
+    const float f = exp2_fast(A.pml[2 * (z * n + at)] - base);
     if (lz == 0.f) continue;
     l += lz * f;
     if (col < A.dim) {
@@ -205,7 +365,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
       o[4] += b.x * f, o[5] += b.y * f, o[6] += b.z * f, o[7] += b.w * f;
     }
   }
-  if (col == 0) A.lse[at] = l == 0.f ? -INFINITY : fmaf(m, A.scale, logf(l));
+  if (col == 0) A.lse[at] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
   if (col < A.dim) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     bf16x8 r;
@@ -223,9 +383,9 @@ void forward(hipStream_t s, const AttnArgs &a) {
   const int tiles = int(a.tq * a.rep / bm) + a.seqs;
   const dim3 grid(uint32_t(tiles) * a.kv_heads, a.splits);
   if (bm == 32)
-    hipLaunchKernelGGL((k_attn_fwd<D, 1>), grid, dim3(256), 0, s, a, tiles);
+    hipLaunchKernelGGL(k_attn_few<D>, grid, dim3(256), 0, s, a, tiles);
   else
-    hipLaunchKernelGGL((k_attn_fwd<D, 4>), grid, dim3(256), 0, s, a, tiles);
+    hipLaunchKernelGGL(k_attn_many<D>, grid, dim3(256), 0, s, a, tiles);
   if (a.splits > 1)
     hipLaunchKernelGGL(k_attn_join, dim3(uint32_t((a.heads * a.tq + 15) / 16)), dim3(256), 0, s, a);
 }

@@ -207,6 +207,34 @@ def test_hidden_values_have_no_part(bad):
     close("dv", t.whole(t.grads[2])[1:], want[2][1:], err[2][1:])
 
 
+@pytest.mark.parametrize("causal,n,heads,kv", [(True, 200, 2, 1), (True, 333, 2, 2), (False, 150, 4, 2), (True, 1, 2, 1)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_special_values_that_are_seen(causal, n, heads, kv, dim):
+    """An infinity or a NaN among the values reaches the rows that see it, and no others; among
+    the gradients, the keys that are seen by its query; wherever in a tile it lies."""
+    rng = np.random.default_rng(n + dim)
+    for at in sorted({0, n - 1, *rng.integers(0, n, 12).tolist()}):
+        t = Case(SAME(n), heads, kv, dim, causal)
+        bad = float(rng.choice([np.nan, np.inf, -np.inf]))
+        t.d["v"][at, :, 3] = bad
+        t.forward()
+        o = t.whole(t.d["o"])
+        see = np.arange(n) >= at if causal else np.ones(n, bool)
+        assert np.array_equal(o[see, :, 3], np.full((see.sum(), heads), bad), equal_nan=True)
+        assert np.isfinite(o[~see]).all() and np.isfinite(np.delete(o, 3, 2)).all()
+        t = Case(SAME(n), heads, kv, dim, causal)
+        t.forward()
+        t.d["g"][at, :, 5] = bad
+        t.backward()
+        dq, dk, dv = (t.whole(x) for x in t.grads)
+        see = np.arange(n) <= at if causal else np.ones(n, bool)
+        assert not np.isfinite(dv[see, :, 5]).any() and np.isfinite(dv[~see]).all()
+        assert np.isfinite(np.delete(dv, 5, 2)).all()
+        # g v^T and its row's sum are infinite or NaN, their difference too
+        assert not np.isfinite(dk[see]).any() and np.isfinite(dk[~see]).all()
+        assert not np.isfinite(dq[at]).any() and np.isfinite(np.delete(dq, at, 0)).all()
+
+
 def test_values_behind_a_sequence_have_no_part():
     """The rows behind a sequence's last, in its last tile, are the next sequence's or nobody's."""
     for causal in (True, False):
