@@ -94,14 +94,11 @@ __device__ __forceinline__ void share(int n, int &begin, int &end) {
   end = int(int64_t(n) * (blockIdx.y + 1) / gridDim.y);
 }
 
-// Four wavefronts of 32 rows.  The keys come by 32 at a time, two to a tile, in three stages that are in the
-// registers together: the scores of the next 32, the exponentials of these, and the product with the
-// values of the last.  The three need nothing of each other, so matrix and vector units work
-// side by side; one stage after the other, a compute unit's two workgroups keep either idle
-// half of the time (16384 tokens, 16/4 heads of 128: TIME_OLD us one after the other, TIME_NEW us so).
+// Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
+// joined at the end.
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attn_many(AttnArgs A, int tiles) {
-  constexpr int BM = 128, BN = 64, T = D / 32, KK = D / 16;
+__global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
+  constexpr int BM = 128, BN = 32, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
@@ -111,7 +108,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_many(AttnArgs A, int tiles) {
   int begin, end;
   share((y.kend + BN - 1) / BN, begin, end);
   const int n = end - begin;
-  y.lim = min(y.lim, end * BN);  // the scores that follow the split's last keys are nobody's
 
   bf16x8 q[KK];
   {
@@ -122,105 +118,64 @@ __global__ __launch_bounds__(256, 2) void k_attn_many(AttnArgs A, int tiles) {
   const Places<D> places;
   const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + kvh * A.hsv;
   const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
-  auto load_k = [&](int it, unsigned char *kt) __attribute__((always_inline)) {
-    kload.load(kt, int64_t(it) * BN, lk - it * BN);
-  };
-  auto load_v = [&](int it, unsigned char *vt) __attribute__((always_inline)) {
-    vload.load(vt, int64_t(it) * BN, lk - it * BN);
-  };
 
-  f32x16 o[T], s;    // s: the scores of the keys whose turn it is
-  bf16x8 p[2];       // probabilities of the last 32, not yet in o
+  f32x16 o[T];
   clear(o);
   Sums z(A.scale * LOG2E);
   unsigned bad = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) p[0][e] = p[1][e] = (__bf16)0.f;
 
-  // s holds the scores of the 32 keys from j on: those that the row does not see become -inf, and
-  // the base is moved if it would let an exponential exceed 2^8 (most tiles leave it)
-  auto meet = [&](int j, auto masked) __attribute__((always_inline)) {
-    const int left = y.lim - j - 4 * (lane >> 5);
+  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const Places<D> at = places.here();
+#pragma unroll
+    for (int sub = 0; sub < BN / 32; ++sub) {
+    const int left = y.lim - (it * BN + sub * 32) - 4 * (lane >> 5);  // keys the row sees from its half's first on
+    f32x16 s[1];
+    clear(s);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) s[0] = mfma(at.rows(kt, sub * 32, kk), q[kk], s[0]);
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if (decltype(masked)::value && 8 * (i / 4) + i % 4 >= left) s[i] = -INFINITY;
-      top = fmaxf(top, s[i]);
+      if (MASKED && 8 * (i / 4) + i % 4 >= left) s[0][i] = -INFINITY;
+      top = fmaxf(top, s[0][i]);
     }
-    if (!z.rises(halves_max(top))) return;
-    const float f = z.move();
+    if (z.rises(halves_max(top))) {
+      const float f = z.move();
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+      for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(float(p[c][e]) * f);  // a power of two: exact
-#pragma unroll
-    for (int t = 0; t < T; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[t][i] *= f;
-  };
-  // o += p v, the values of 32 rows of a tile
-  auto product = [&](const Places<D> &at, const unsigned char *vt, int first, auto masked) __attribute__((always_inline)) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if constexpr (decltype(masked)::value) add_rows_finite<D>(o, at, vt, first + 16 * c, p[c], bad);
-      else add_rows<D>(o, at, vt, first + 16 * c, p[c]);
+        for (int i = 0; i < 16; ++i) o[t][i] *= f;
     }
-  };
-  // one turn: scores of the 32 rows of `kt` from kfirst on (the keys from j on), exponentials of s,
-  // the product of p with the rows of `vt` from vfirst on
-  auto turn = [&](int j, const unsigned char *kt, int kfirst, const unsigned char *vt, int vfirst, auto masked)
-      __attribute__((always_inline)) {
-    const Places<D> at = places.here();
-    f32x16 next[1];
-    clear(next);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) next[0] = mfma(at.rows(kt, kfirst, kk), q[kk], next[0]);
-    product(at, vt, vfirst, masked);
-    float l0 = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = z.exponential(s[i]);
-      l0 += s[i];
+      s[0][i] = z.exponential(s[0][i]);
+      z.l += s[0][i];
     }
-    z.l += l0;
-    p[0] = operand(s, 0);
-    p[1] = operand(s, 1);
-    s = next[0];
-  };
-
-  if (n > 0) {
-    load_k(begin, kt0);
-    // what p multiplies before there are values
-    for (int e = threadIdx.x; e < BN * D * 2 / 16; e += 256) reinterpret_cast<u32x4 *>(vt1)[e] = u32x4{0u, 0u, 0u, 0u};
-    tile_barrier();
-    load_v(begin, vt0);
-    if (n > 1) load_k(begin + 1, kt1);
-    const Places<D> at = places.here();
-    clear(*reinterpret_cast<f32x16(*)[1]>(&s));
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) s = mfma(at.rows(kt0, 0, kk), q[kk], s);
-    meet(begin * BN, std::true_type());
-  }
-  // Tiles which every row of the wavefront sees whole, and the next one too, are met without tests.
-  const int full = max(0, min(n, y.lim_lo / BN - begin) - 1) & ~1;
+    for (int c = 0; c < 2; ++c) {
+      if constexpr (MASKED) add_rows_finite<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c), bad);
+      else add_rows<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c));
+    }
+    }
+  };
+  // tiles whose keys (the wavefront's quarter) every row sees
+  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;
+  auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+    kload.load(kt, int64_t(it) * BN, lk - it * BN);
+    vload.load(vt, int64_t(it) * BN, lk - it * BN);
+  };
+  if (n > 0) load(begin, kt0, vt0);
   two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
-    const int it = begin + i;
-    unsigned char *const kt = place ? kt1 : kt0, *const kn = place ? kt0 : kt1, *const vt = place ? vt1 : vt0,
-                        *const vn = place ? vt0 : vt1;
-    // the tile's second scores; the values of the last tile's second half
-    turn(it * BN + 32, kt, 32, vn, 32, masked);
-    meet(it * BN + 32, masked);
-    tile_barrier();  // this tile's values and the next one's keys are there; their predecessors may go
-    if (i + 2 < n) load_k(it + 2, kt);
-    if (i + 1 < n) load_v(it + 1, vn);
-    turn(it * BN + 64, kn, 0, vt, 0, masked);
-    meet(it * BN + 64, masked);
+    tile_barrier();
+    if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
+    work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
-  if (n > 0) product(places.here(), (n - 1) & 1 ? vt1 : vt0, 32, std::true_type());
-  // clamped were the values from the second half of the last tile met without tests on
   if (__any(bad != 0))
-    add_special<D>(o, vp, A.ldv, A.dim, (begin + full) * BN - (full ? 32 : 0), min(end * BN, lk), false,
-                   [&](int j) { return j < y.lim; });
+    for (int it = begin + full; it < end; ++it)
+      add_special<D>(o, vp, A.ldv, A.dim, it * BN, min(it * BN + BN, lk), false,
+                     [&](int j) { return j < y.lim; });
+
   if (y.valid) finish<D>(A, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
 }
 
