@@ -128,7 +128,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   __shared__ __align__(16) unsigned char vt[BM * D * 2];
   __shared__ __align__(16) float st0[128], st1[128];  // lse in base 2 | delta, 64 places each
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
+  // a tile's heads and their parts side by side: workgroups start in the order of their work
+  const int part = blockIdx.x % A.parts, kvh = blockIdx.x / A.parts % A.kv_heads, tile = int(blockIdx.x / A.parts / A.kv_heads);
   Sequence sq;
   if (!find_tile<false>(A, 1, BM, 0, tile, sq)) return;
   const int first = int(sq.first), key = first + wave * 32 + (lane & 31);
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   // the first query that sees the key, and the workgroup's first tile
   const int from = A.causal ? max(0, key - past) : 0;
   const int begin = (A.causal ? max(0, first - past) : 0) / BN, end = (sq.lq + BN - 1) / BN;
-  const int heads = A.rep / A.parts, head0 = kvh * A.rep + int(blockIdx.y) * heads;
+  const int heads = A.rep / A.parts, head0 = kvh * A.rep + part * heads;
   const int per = max(0, end - begin), n = per * heads;  // tiles of a head, of all
 
   bf16x8 k[KK];
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   if (!valid) return;
   if (A.parts > 1) {
     // fp32, for k_attn_heads: dk's parts, then dv's
-    float *const p = A.pkv + ((int64_t(blockIdx.y) * A.tk + sq.k0 + key) * A.kv_heads + kvh) * A.dim;
+    float *const p = A.pkv + ((int64_t(part) * A.tk + sq.k0 + key) * A.kv_heads + kvh) * A.dim;
     store_part<D>(p, dk, A.scale, A.dim);
     store_part<D>(p + A.parts * A.tk * A.kv_heads * A.dim, dv, 1.f, A.dim);
     return;
@@ -282,7 +283,7 @@ template <int D>
 void backward(hipStream_t s, const AttnArgs &a) {
   const int kt = int(a.tk / 128) + a.seqs, qt = int(a.tq * a.rep / 128) + a.seqs;
   if (a.tk > 0) {
-    hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads, a.parts), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads * a.parts), dim3(256), 0, s, a);
     if (a.parts > 1)
       hipLaunchKernelGGL(k_attn_heads, dim3(uint32_t((a.tk * a.kv_heads * (a.dim / 8) + 255) / 256), 2), dim3(256), 0, s,
                          a);

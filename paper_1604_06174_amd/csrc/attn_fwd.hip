@@ -69,14 +69,31 @@ struct Query {
   }
 };
 
+// What a workgroup does: a tile's heads and their splits lie side by side, so that workgroups start in
+// the order of their work.
+struct Block {
+  int split, kvh, tile;
+
+  __device__ __forceinline__ explicit Block(const AttnArgs &A) {
+    split = int(blockIdx.x % A.splits);
+    kvh = int(blockIdx.x / A.splits % A.kv_heads);
+    tile = int(blockIdx.x / A.splits / A.kv_heads);
+  }
+  // the split's share of n tiles
+  __device__ __forceinline__ void share(const AttnArgs &A, int n, int &begin, int &end) const {
+    begin = int(int64_t(n) * split / A.splits);
+    end = int(int64_t(n) * (split + 1) / A.splits);
+  }
+};
+
 // o (unscaled) and the sums of a lane's row to their places: o / l and lse, or the parts of a split
 template <int D>
-__device__ __forceinline__ void finish(const AttnArgs &A, int head, int64_t token, const f32x16 (&o)[D / 32], float base,
+__device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, int64_t token, const f32x16 (&o)[D / 32], float base,
                                        float l) {
   const int64_t at_row = head * A.tq + token;
   const bool first = (threadIdx.x & 63) < 32;
-  if (gridDim.y > 1) {
-    const int64_t p = int64_t(blockIdx.y) * A.heads * A.tq + at_row;
+  if (A.splits > 1) {
+    const int64_t p = int64_t(split) * A.heads * A.tq + at_row;
     if (first) {
       A.pml[2 * p] = base;
       A.pml[2 * p + 1] = l;
@@ -88,12 +105,6 @@ __device__ __forceinline__ void finish(const AttnArgs &A, int head, int64_t toke
   store_row<D>(A.o + token * A.ldo + head * A.hso, o, l == 0.f ? 0.f : 1.f / l, A.dim);
 }
 
-// the split's share of n tiles
-__device__ __forceinline__ void share(int n, int &begin, int &end) {
-  begin = int(int64_t(n) * blockIdx.y / gridDim.y);
-  end = int(int64_t(n) * (blockIdx.y + 1) / gridDim.y);
-}
-
 // Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
 // joined at the end.
 template <int D>
@@ -101,12 +112,12 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   constexpr int BM = 128, BN = 32, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
+  const Block b(A);
   Query<BM> y;
-  if (!y.find(A, tiles, tile, kvh, wave * 32 + (lane & 31))) return;
+  if (!y.find(A, tiles, b.tile, b.kvh, wave * 32 + (lane & 31))) return;
   const int lk = y.sq.lk;
   int begin, end;
-  share((y.kend + BN - 1) / BN, begin, end);
+  b.share(A, (y.kend + BN - 1) / BN, begin, end);
   const int n = end - begin;
 
   bf16x8 q[KK];
@@ -116,8 +127,8 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
     for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
   }
   const Places<D> places;
-  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + kvh * A.hsv;
-  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
+  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
 
   f32x16 o[T];
   clear(o);
@@ -176,7 +187,7 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
       add_special<D>(o, vp, A.ldv, A.dim, it * BN, min(it * BN + BN, lk), false,
                      [&](int j) { return j < y.lim; });
 
-  if (y.valid) finish<D>(A, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
+  if (y.valid) finish<D>(A, b.split, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
 }
 
 // Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
@@ -186,12 +197,12 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   constexpr int BM = 32, BN = 128, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % A.kv_heads, tile = int(blockIdx.x / A.kv_heads);
+  const Block b(A);
   Query<BM> y;
-  if (!y.find(A, tiles, tile, kvh, lane & 31)) return;
+  if (!y.find(A, tiles, b.tile, b.kvh, lane & 31)) return;
   const int lk = y.sq.lk;
   int begin, end;
-  share((y.kend + BN - 1) / BN, begin, end);
+  b.share(A, (y.kend + BN - 1) / BN, begin, end);
   const int n = end - begin;
 
   bf16x8 q[KK];
@@ -201,8 +212,8 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
     for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
   }
   const Places<D> places;
-  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + kvh * A.hsv;
-  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
+  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
 
   f32x16 o[T];
   clear(o);
@@ -288,11 +299,11 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int e = (32 * t + d_row(i)) * 32 + (lane & 31);
-      const float *const a = reinterpret_cast<const float *>(kt0) + e, *const b = reinterpret_cast<const float *>(vt0) + e;
+      const float *const k = reinterpret_cast<const float *>(kt0) + e, *const v = reinterpret_cast<const float *>(vt0) + e;
       // a wavefront without keys has a factor of 0 and nothing but zeros
-      o[t][i] = a[0] * f[0] + a[D * 32] * f[1] + b[0] * f[2] + b[D * 32] * f[3];
+      o[t][i] = k[0] * f[0] + k[D * 32] * f[1] + v[0] * f[2] + v[D * 32] * f[3];
     }
-  if (y.valid) finish<D>(A, y.head, y.sq.q0 + y.token, o, base, sum);
+  if (y.valid) finish<D>(A, b.split, y.head, y.sq.q0 + y.token, o, base, sum);
 }
 
 // a row's splits joined: sixteen lanes a row, eight columns each
@@ -336,7 +347,7 @@ template <int D>
 void forward(hipStream_t s, const AttnArgs &a) {
   const int bm = few_rows(a) ? 32 : 128;
   const int tiles = int(a.tq * a.rep / bm) + a.seqs;
-  const dim3 grid(uint32_t(tiles) * a.kv_heads, a.splits);
+  const dim3 grid(uint32_t(tiles) * a.kv_heads * a.splits);
   if (bm == 32)
     hipLaunchKernelGGL(k_attn_few<D>, grid, dim3(256), 0, s, a, tiles);
   else
