@@ -256,22 +256,32 @@ __device__ __forceinline__ void in_turn(L &&load, U &&use) {
   }
 }
 
-// magnitudes above the largest finite one as that one (as pairs of 16 bits without the sign,
-// infinities and NaNs are the larger numbers); `bad` is not 0 if there were any
-__device__ __forceinline__ bf16x8 finite(bf16x8 a, unsigned &bad) {
+// Magnitudes above the largest finite one in a tile as that one (as pairs of 16 bits without the
+// sign, infinities and NaNs are the larger numbers); `special` is set if there were any.  A product
+// with a tile of which a row does not see all takes zeros for what is hidden, and an infinity or a NaN would
+// make a NaN of them; add_special then gives them to the rows that see them.  All of the workgroup, between
+// barriers.
+template <int BYTES>
+__device__ __forceinline__ void scrub(unsigned char *tile, int &special) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   const u16x2 most = {0x7f7f, 0x7f7f};
-  u32x4 w = __builtin_bit_cast(u32x4, a);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const u16x2 m = __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu);
-    const unsigned f = __builtin_bit_cast(unsigned, __builtin_elementwise_min(m, most)) | (w[k] & 0x80008000u);
-    bad |= f ^ w[k];
-    w[k] = f;
+  for (int c = 0; c < BYTES / 4096; ++c) {
+    u32x4 *const at = reinterpret_cast<u32x4 *>(tile) + c * 256 + threadIdx.x;
+    u32x4 w = *at;
+    unsigned changed = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const u16x2 m = __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu);
+      const unsigned f = __builtin_bit_cast(unsigned, __builtin_elementwise_min(m, most)) | (w[k] & 0x80008000u);
+      changed |= f ^ w[k];
+      w[k] = f;
+    }
+    if (changed) {
+      *at = w;
+      special = 1;
+    }
   }
-  // here and now: added up at a block's end, these would keep all the values until then
-  asm volatile("" : "+v"(bad));
-  return __builtin_bit_cast(bf16x8, w);
 }
 
 // acc += (values of the 16 rows of the tile from `first` on, transposed) b
@@ -282,18 +292,8 @@ __device__ __forceinline__ void add_rows(f32x16 (&acc)[D / 32], const Places<D> 
   for (int t = 0; t < D / 32; ++t) acc[t] = mfma(at.columns(tile, first, t), b, acc[t]);
 }
 
-// The same where b is zero for rows that the lane's row does not see: an infinity or a NaN in
-// such a row would make a NaN of the zero, so only finite values are taken (finite(), above), and
-// add_special then gives the others to the lanes that see them.
-template <int D>
-__device__ __forceinline__ void add_rows_finite(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
-                                                int first, bf16x8 b, unsigned &bad) {
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t) acc[t] = mfma(finite(at.columns(tile, first, t), bad), b, acc[t]);
-}
-
-// What add_rows_finite left out: rows row0 .. row1 - 1 of a matrix whose row r is at src +
-// r ld; sees(r): does the lane's row see it?  A probability times an infinity or a NaN is that
+// What scrub took out of rows row0 .. row1 - 1 of a matrix whose row r is at src + r ld; sees(r): does
+// the lane's row see it?  A probability times an infinity or a NaN is that
 // infinity or NaN (it is positive, however small); a score's gradient times one is a NaN, for
 // the score itself is then infinite or NaN (nan = true).
 template <int D, typename F>

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   const int token = int(r / A.rep), head = kvh * A.rep + int(r - int64_t(token) * A.rep);
   const int past = sq.lk - sq.lq;
   const int lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;
-  const int lim_lo = __builtin_amdgcn_readfirstlane(lim);
+  const int lim_lo = A.causal ? min(sq.lk, max(0, int(sq.first / A.rep) + past + 1)) : sq.lk;  // the workgroup's least
   const int64_t last = min(sq.first + BM, rows) - 1;
   const int kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
   const int end = (kend + BN - 1) / BN;
@@ -75,7 +75,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
     kload.load(kt, int64_t(it) * BN, sq.lk - it * BN);
     vload.load(vt, int64_t(it) * BN, sq.lk - it * BN);
   };
-  unsigned bad = 0;
+  __shared__ int special;
+  if (threadIdx.x == 0) special = 0;
   f32x16 dq[T];
   clear(dq);
   const float sc = A.scale * LOG2E;
@@ -101,17 +102,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
       }
       const bf16x8 ds[2] = {operand(s[0], 0), operand(s[0], 1)};
       in_turn<2 * T, 4>([&](int i) { return at.columns(kt, u * 32 + i / T * 16, i % T); },
-                        [&](int i, bf16x8 a) { dq[i % T] = mfma(MASKED ? finite(a, bad) : a, ds[i / T], dq[i % T]); });
+                        [&](int i, bf16x8 a) { dq[i % T] = mfma(a, ds[i / T], dq[i % T]); });
     }
   };
   if (end > 0) load(0, kt0, vt0);
-  const int full = min(end, lim_lo / BN) & ~1;  // tiles that every row of the wavefront sees whole
+  const int full = min(end, lim_lo / BN) & ~1;  // tiles that every row sees whole
   two_kinds(end, full, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
+    if constexpr (decltype(masked)::value) {
+      scrub<BN * D * 2>(place ? kt1 : kt0, special);
+      __syncthreads();
+    }
     if (it + 1 < end) load(it + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(it, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
-  if (__any(bad != 0))
+  if (end > 0 && special)
     add_special<D>(dq, kp, A.ldk, A.dim, full * BN, min(end * BN, sq.lk), true, [&](int j) { return j < lim; });
   if (valid) store_row<D>(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
 }
@@ -167,7 +172,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   f32x16 dk[T], dv[T];
   clear(dk);
   clear(dv);
-  unsigned badq = 0, badg = 0;
+  __shared__ int special;
+  if (threadIdx.x == 0) special = 0;
 
   auto work = [&](int t0, const unsigned char *qt, const unsigned char *gt, const float *st, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
@@ -201,9 +207,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
       }
       const bf16x8 pb[2] = {operand(s[0], 0), operand(s[0], 1)}, ds[2] = {operand(dp[0], 0), operand(dp[0], 1)};
       in_turn<2 * T, 4>([&](int i) { return at.columns(gt, u * 32 + i / T * 16, i % T); },
-                        [&](int i, bf16x8 a) { dv[i % T] = mfma(MASKED ? finite(a, badg) : a, pb[i / T], dv[i % T]); });
+                        [&](int i, bf16x8 a) { dv[i % T] = mfma(a, pb[i / T], dv[i % T]); });
       in_turn<2 * T, 4>([&](int i) { return at.columns(qt, u * 32 + i / T * 16, i % T); },
-                        [&](int i, bf16x8 a) { dk[i % T] = mfma(MASKED ? finite(a, badq) : a, ds[i / T], dk[i % T]); });
+                        [&](int i, bf16x8 a) { dk[i % T] = mfma(a, ds[i / T], dk[i % T]); });
     }
   };
   // Tiles from the last query back: workgroups that start together read the same tiles together
@@ -231,11 +237,16 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
   const int whole = (end - seen) * heads;  // tiles that see all of the workgroup's keys
   two_kinds(n, whole & ~1, [&](int it, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
+    if constexpr (decltype(masked)::value) {
+      scrub<BN * D * 2>(place ? qt1 : qt0, special);
+      scrub<BN * D * 2>(place ? gt1 : gt0, special);
+      __syncthreads();
+    }
     if (it + 1 < n) next(place ? qt0 : qt1, place ? gt0 : gt1, place ? st0 : st1);
     work(now.t * BN, place ? qt1 : qt0, place ? gt1 : gt0, place ? st1 : st0, masked);
     advance(now);
   });
-  if (__any((badq | badg) != 0))
+  if (n > 0 && special)
     for (int h = 0; h < heads; ++h) {
       auto sees = [&](int r) { return r >= from; };
       // the tiles with tests: an odd one of the others, which comes just before them, is taken so too

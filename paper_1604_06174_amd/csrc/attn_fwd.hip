@@ -48,8 +48,7 @@ struct Query {
   Sequence sq;
   int64_t rows;
   int token, head, lim;  // lim: keys it sees
-  int lim_lo;            // the wavefront's least
-  int kend;              // the workgroup's most
+  int lim_lo, kend;      // the workgroup's least and most
   bool valid;
 
   // the lane's row is `row` of the tile; false: the tile has none
@@ -62,8 +61,8 @@ struct Query {
     head = kvh * A.rep + int(r - int64_t(token) * A.rep);
     const int past = sq.lk - sq.lq;
     lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;
-    lim_lo = __builtin_amdgcn_readfirstlane(lim);
     const int64_t last = min(sq.first + BM, rows) - 1;
+    lim_lo = A.causal ? min(sq.lk, max(0, int(sq.first / A.rep) + past + 1)) : sq.lk;
     kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
     return true;
   }
@@ -133,7 +132,8 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   f32x16 o[T];
   clear(o);
   Sums z(A.scale * LOG2E);
-  unsigned bad = 0;
+  __shared__ int special;
+  if (threadIdx.x == 0) special = 0;
 
   auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
@@ -164,14 +164,10 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
       z.l += s[0][i];
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if constexpr (MASKED) add_rows_finite<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c), bad);
-      else add_rows<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c));
-    }
+    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c));
     }
   };
-  // tiles whose keys (the wavefront's quarter) every row sees
-  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;
+  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;  // tiles that every row sees whole
   auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
     kload.load(kt, int64_t(it) * BN, lk - it * BN);
     vload.load(vt, int64_t(it) * BN, lk - it * BN);
@@ -179,13 +175,15 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   if (n > 0) load(begin, kt0, vt0);
   two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
+    if constexpr (decltype(masked)::value) {
+      scrub<BN * D * 2>(place ? vt1 : vt0, special);
+      __syncthreads();
+    }
     if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
-  if (__any(bad != 0))
-    for (int it = begin + full; it < end; ++it)
-      add_special<D>(o, vp, A.ldv, A.dim, it * BN, min(it * BN + BN, lk), false,
-                     [&](int j) { return j < y.lim; });
+  if (n > 0 && special)
+    add_special<D>(o, vp, A.ldv, A.dim, (begin + full) * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
 
   if (y.valid) finish<D>(A, b.split, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
 }
@@ -218,7 +216,8 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   f32x16 o[T];
   clear(o);
   Sums z(A.scale * LOG2E);
-  unsigned bad = 0;
+  __shared__ int special;
+  if (threadIdx.x == 0) special = 0;
 
   auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
@@ -247,14 +246,9 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
       z.l += s[0][i];
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if constexpr (MASKED) add_rows_finite<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c), bad);
-      else add_rows<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c));
-    }
+    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c));
   };
-  // tiles whose keys (the wavefront's quarter) every row sees
-  const int whole = y.lim_lo - (wave + 1) * 32 + BN;
-  const int full = max(0, min(n, (whole > 0 ? whole / BN : 0) - begin)) & ~1;
+  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;  // tiles that every row sees whole
   auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
     kload.load(kt, int64_t(it) * BN, lk - it * BN);
     vload.load(vt, int64_t(it) * BN, lk - it * BN);
@@ -262,10 +256,14 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   if (n > 0) load(begin, kt0, vt0);
   two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
+    if constexpr (decltype(masked)::value) {
+      scrub<BN * D * 2>(place ? vt1 : vt0, special);
+      __syncthreads();
+    }
     if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
-  if (__any(bad != 0))
+  if (n > 0 && special)
     for (int it = begin + full; it < end; ++it)
       add_special<D>(o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
                      [&](int j) { return j < y.lim; });
