@@ -113,7 +113,8 @@ __device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int size, 
     const bool has = lo >= low && lo < low + n;
     const uint64_t all = __ballot(has);
     const int who = __ffsll((unsigned long long)__ballot(has && __popcll(all & ((1ull << lane) - 1)) == rank)) - 1;
-    rows_of(A, who, q);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, who); };
+    q = Sequence{of(int(mine.q0)), of(int(mine.k0)), of(mine.lq), of(mine.lk), 0};  // rows fit 32 bits
     const int t = lo - __builtin_amdgcn_readlane(low, who);
     q.first = int64_t(QUERIES ? t : __builtin_amdgcn_readlane(n, who) - 1 - t) * size;
     return true;
@@ -156,13 +157,13 @@ struct Loader {
   const char *src;  // row 0
   int64_t pitch;    // bytes from row to row
   unsigned place;   // the lane's first chunk from the tile's first row, in bytes
-  bool in, whole;   // its columns are below dim; all lanes' are, and 32 bits hold their places
+  int dim;
+  bool whole;       // all columns are below dim, and 32 bits hold the places
 
-  __device__ __forceinline__ Loader(const __bf16 *base, int64_t ld, int dim)
-      : src(reinterpret_cast<const char *>(base)), pitch(2 * ld) {
+  __device__ __forceinline__ Loader(const __bf16 *base, int64_t ld, int dim_)
+      : src(reinterpret_cast<const char *>(base)), pitch(2 * ld), dim(dim_) {
     const int row = threadIdx.x / C, col = ((threadIdx.x % C) ^ swizzle<D>(row)) * 8;
     place = unsigned(row) * unsigned(pitch) + 2 * col;
-    in = col < dim;
     whole = dim == D && pitch < (1 << 24);
   }
   // the tile from row `first` on, `offset` bytes further
@@ -177,12 +178,14 @@ struct Loader {
         __builtin_amdgcn_global_load_lds(q + place, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
       }
     } else {
-      const int row = threadIdx.x / C, col = ((threadIdx.x % C) ^ swizzle<D>(row)) * 8;
+      int tid = threadIdx.x;
+      asm volatile("" : "+v"(tid));  // what follows is rare: it is worked out here, not kept in registers
+      const int row = tid / C, col = ((tid % C) ^ swizzle<D>(row)) * 8;
 #pragma unroll
       for (int c = 0; c < N; ++c) {
-        const bool ok = in && row + c * STEP < valid;
+        const bool ok = col < dim && row + c * STEP < valid;
         const void *const q = ok ? static_cast<const void *>(p + (row + c * STEP) * pitch + 2 * col)
-                                 : g_zeros + 4 * (threadIdx.x & 255);
+                                 : g_zeros + 4 * (tid & 255);
         __builtin_amdgcn_global_load_lds(q, (lds_void *)(to + c * THREADS * 16), 16, 0, 0);
       }
     }

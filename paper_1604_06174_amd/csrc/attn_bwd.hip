@@ -1,9 +1,9 @@
 // Attention backward over packed sequences, from the forward's o and lse:
 //   p = exp(scale q k^T - lse), ds = p (g v^T - delta), delta = sum(g o),
 //   dq = scale ds k, dk = scale ds^T q, dv = p^T g.
-// Two passes, so that nothing is added by atomics: k_attn_dkv keeps 32 keys a wavefront and lets
-// the queries come by, k_attn_dq keeps 32 queries and lets the keys come by (p and ds
-// are formed in both: seven products instead of five).
+// Two passes, so that nothing is added by atomics: k_attn_dq keeps 32 queries a wavefront and lets
+// the keys come by, k_attn_dkv keeps 32 keys and lets the queries come by (p and ds are formed in
+// both: seven products instead of five).
 #include "attn.h"
 #include "common.h"
 
@@ -11,32 +11,6 @@ namespace ckpt {
 namespace {
 
 using namespace at;
-
-// delta, and lse in base 2 (infinite for rows that see nothing, so that p = exp2(-inf)); sixteen
-// lanes a row, eight columns each
-__global__ __launch_bounds__(256) void k_attn_delta(AttnArgs A) {
-  const int64_t at = blockIdx.x * int64_t(16) + threadIdx.x / 16;
-  if (at >= A.heads * A.tq) return;
-  const int64_t token = at / A.heads;
-  const int head = int(at - token * A.heads), col = (threadIdx.x & 15) * 8;
-  if (token < A.qoff[0] || token >= A.qoff[A.seqs]) return;
-  float s = 0.f;
-  if (col < A.dim) {
-    const int64_t e = token * A.ldo + head * A.hso + col;
-    const bf16x8 g = *reinterpret_cast<const bf16x8 *>(A.g + e), o = *reinterpret_cast<const bf16x8 *>(A.out + e);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s = fmaf(float(g[k]), float(o[k]), s);
-  }
-  s = xor_add<1>(s);
-  s = xor_add<2>(s);
-  s = xor_add<4>(s);
-  s = xor_add<8>(s);
-  if (col == 0) {
-    const float lse = A.lse[head * A.tq + token];
-    A.delta[head * A.tq + token] = s;
-    A.lse2[head * A.tq + token] = lse == -INFINITY ? INFINITY : lse * LOG2E;
-  }
-}
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
@@ -67,7 +41,25 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
       g[kk] = kept(pg, kk, A.dim);
     }
   }
-  const float lse2 = A.lse2[head * A.tq + sq.q0 + token], delta = A.delta[head * A.tq + sq.q0 + token];
+  // the row's sum of g o and its lse in base 2 (infinite for rows that see nothing, so that p = exp2(-inf)),
+  // for here and for k_attn_dkv
+  const int64_t at_row = head * A.tq + sq.q0 + token;
+  float lse2 = A.lse[at_row], delta = 0.f;
+  lse2 = lse2 == -INFINITY ? INFINITY : lse2 * LOG2E;
+  {
+    const __bf16 *p = A.out + (sq.q0 + token) * A.ldo + head * A.hso;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const bf16x8 o = kept(p, kk, A.dim);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(float(g[kk][e]), float(o[e]), delta);
+    }
+    delta = halves_add(delta);
+    if (valid && lane < 32) {
+      A.lse2[at_row] = lse2;
+      A.delta[at_row] = delta;
+    }
+  }
   const Places<D> places;
   const __bf16 *const kp = A.k + sq.k0 * A.ldk + kvh * A.hsk;
   const Loader<D, BN, 256> kload(kp, A.ldk, A.dim), vload(A.v + sq.k0 * A.ldv + kvh * A.hsv, A.ldv, A.dim);
@@ -127,8 +119,8 @@ static __device__ __align__(16) const float g_infinity[64] = {
     CKPT_INF16, CKPT_INF16, CKPT_INF16, CKPT_INF16};
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
-  constexpr int BM = 128, BN = D == 128 ? 32 : 64, T = D / 32, KK = D / 16;
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {
+  constexpr int BM = 128, BN = 32, T = D / 32, KK = D / 16;
   __shared__ __align__(16) unsigned char qt0[BN * D * 2], qt1[BN * D * 2], gt0[BN * D * 2], gt1[BN * D * 2];
   __shared__ __align__(16) unsigned char vt[BM * D * 2];
   __shared__ __align__(16) float st0[128], st1[128];  // lse in base 2 | delta, 64 places each
@@ -160,13 +152,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs A) {
     const int t0 = t * BN;
     qload.load(qt, t0, sq.lq - t0, 2 * h * A.hsq);
     gload.load(gt, t0, sq.lq - t0, 2 * h * A.hso);
-    // a wavefront each; rows past the sequence's: p = exp2(-inf)
+    // lse and delta, a wavefront each
     if (wave < 2) {
-      const bool ok = t0 + lane < sq.lq && lane < BN;
-      const int64_t e = (head0 + h) * A.tq + sq.q0 + t0 + lane;
-      const float *const none = wave ? reinterpret_cast<const float *>(g_zeros) + lane : g_infinity + lane;
-      const float *const p = ok ? (wave ? A.delta : A.lse2) + e : none;
-      __builtin_amdgcn_global_load_lds(p, (lds_void *)(st + 64 * wave), 4, 0, 0);
+      const float *src = (wave ? A.delta : A.lse2) + (head0 + h) * A.tq + sq.q0 + t0;
+      if (t0 + BN <= sq.lq) {
+        asm("" : "+s"(src));
+        const char *const p = reinterpret_cast<const char *>(src);
+        __builtin_amdgcn_global_load_lds(p + unsigned(4 * (lane & (BN - 1))), (lds_void *)(st + 64 * wave), 4, 0, 0);
+      } else {  // rows past the sequence's: p = exp2(-inf)
+        int at = lane;
+        asm volatile("" : "+v"(at));
+        const float *const none = (wave ? reinterpret_cast<const float *>(g_zeros) : g_infinity) + at;
+        const float *const p = t0 + at < sq.lq ? src + at : none;
+        __builtin_amdgcn_global_load_lds(p, (lds_void *)(st + 64 * wave), 4, 0, 0);
+      }
     }
   };
   f32x16 dk[T], dv[T];
@@ -293,13 +292,11 @@ __global__ __launch_bounds__(256) void k_attn_heads(AttnArgs A) {
 template <int D>
 void backward(hipStream_t s, const AttnArgs &a) {
   const int kt = int(a.tk / 128) + a.seqs, qt = int(a.tq * a.rep / 128) + a.seqs;
-  if (a.tk > 0) {
-    hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads * a.parts), dim3(256), 0, s, a);
-    if (a.parts > 1)
-      hipLaunchKernelGGL(k_attn_heads, dim3(uint32_t((a.tk * a.kv_heads * (a.dim / 8) + 255) / 256), 2), dim3(256), 0, s,
-                         a);
-  }
   if (a.tq > 0) hipLaunchKernelGGL(k_attn_dq<D>, dim3(uint32_t(qt) * a.kv_heads), dim3(256), 0, s, a, qt);
+  if (a.tk == 0) return;
+  hipLaunchKernelGGL(k_attn_dkv<D>, dim3(uint32_t(kt) * a.kv_heads * a.parts), dim3(256), 0, s, a);
+  if (a.parts > 1)
+    hipLaunchKernelGGL(k_attn_heads, dim3(uint32_t((a.tk * a.kv_heads * (a.dim / 8) + 255) / 256), 2), dim3(256), 0, s, a);
 }
 
 }  // namespace
@@ -338,8 +335,6 @@ uint64_t attn_plan(AttnArgs &a, bool backward, char *ws) {
 }
 
 void attn_backward(hipStream_t s, const AttnArgs &a) {
-  if (a.tq > 0)
-    hipLaunchKernelGGL(k_attn_delta, dim3(uint32_t((a.heads * a.tq + 15) / 16)), dim3(256), 0, s, a);
   a.dim <= 64 ? backward<64>(s, a) : backward<128>(s, a);
 }
 
