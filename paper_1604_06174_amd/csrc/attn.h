@@ -98,7 +98,10 @@ __device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int size, 
     if (lane < A.seqs) rows_of(A, lane, mine);
     const int n = int((int64_t(QUERIES ? mine.lq : mine.lk) * per + size - 1) / size);
     const int low = QUERIES && A.causal ? int(int64_t(max(0, mine.lk - mine.lq)) * per / size) : 0;
-    auto above = [&](int w) { return wave_add(max(0, min(n, low + n - w))); };
+    const bool single = !__any(n > 1);  // then a level's tiles are counted without adding up
+    auto above = [&](int w) {
+      return single ? int(__popcll(__ballot(n > 0 && low >= w))) : wave_add(max(0, min(n, low + n - w)));
+    };
     const int total = above(0);
     if (index >= total) return false;
     int lo = 0, hi = 1;
@@ -338,34 +341,34 @@ __device__ __forceinline__ void two_kinds(int n, int n1, F &&step) {
   }
 }
 
-// an accumulator's column, scaled, to a row of 16-bit values
-template <int D>
-__device__ __forceinline__ void store_row(__bf16 *row, const f32x16 (&acc)[D / 32], float scale, int dim) {
+// columns 32 t .. 32 t + 31 of a lane's row from an accumulator, scaled
+__device__ __forceinline__ void store_tile(__bf16 *row, const f32x16 &acc, int t, float scale, int dim) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t)
+  for (int b = 0; b < 4; ++b) {
+    const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
+    if (col >= dim) continue;
+    bf16x4 v;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
-      if (col >= dim) continue;
-      bf16x4 v;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[t][4 * b + k] * scale);
-      *reinterpret_cast<bf16x4 *>(row + col) = v;
-    }
+    for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[4 * b + k] * scale);
+    *reinterpret_cast<bf16x4 *>(row + col) = v;
+  }
 }
 
-template <int D>
-__device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[D / 32], float scale, int dim) {
+__device__ __forceinline__ void store_tile(float *row, const f32x16 &acc, int t, float scale, int dim) {
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t)
+  for (int b = 0; b < 4; ++b) {
+    const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
+    if (col < dim)
+      *reinterpret_cast<float4 *>(row + col) =
+          make_float4(acc[4 * b] * scale, acc[4 * b + 1] * scale, acc[4 * b + 2] * scale, acc[4 * b + 3] * scale);
+  }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[N], float scale, int dim) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int col = 32 * t + 8 * b + 4 * ((threadIdx.x & 63) >> 5);
-      if (col < dim)
-        *reinterpret_cast<float4 *>(row + col) = make_float4(acc[t][4 * b] * scale, acc[t][4 * b + 1] * scale,
-                                                             acc[t][4 * b + 2] * scale, acc[t][4 * b + 3] * scale);
-    }
+  for (int t = 0; t < N; ++t) store_tile(row, acc[t], t, scale, dim);
 }
 
 template <int N>

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   });
   if (end > 0 && special)
     add_special<D>(dq, kp, A.ldk, A.dim, full * BN, min(end * BN, sq.lk), true, [&](int j) { return j < lim; });
-  if (valid) store_row<D>(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
+  if (valid) store_row(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
 }
 
 static __device__ __align__(16) const float g_infinity[64] = {
@@ -257,12 +257,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {
   if (A.parts > 1) {
     // fp32, for k_attn_heads: dk's parts, then dv's
     float *const p = A.pkv + ((int64_t(part) * A.tk + sq.k0 + key) * A.kv_heads + kvh) * A.dim;
-    store_part<D>(p, dk, A.scale, A.dim);
-    store_part<D>(p + A.parts * A.tk * A.kv_heads * A.dim, dv, 1.f, A.dim);
+    store_row(p, dk, A.scale, A.dim);
+    store_row(p + A.parts * A.tk * A.kv_heads * A.dim, dv, 1.f, A.dim);
     return;
   }
-  store_row<D>(A.dk + (sq.k0 + key) * A.ldk + kvh * A.hsk, dk, A.scale, A.dim);
-  store_row<D>(A.dv + (sq.k0 + key) * A.ldv + kvh * A.hsv, dv, 1.f, A.dim);
+  store_row(A.dk + (sq.k0 + key) * A.ldk + kvh * A.hsk, dk, A.scale, A.dim);
+  store_row(A.dv + (sq.k0 + key) * A.ldv + kvh * A.hsv, dv, 1.f, A.dim);
 }
 
 // the parts of the query heads that share a key head, added up in order; a thread has eight columns

@@ -85,23 +85,24 @@ struct Block {
   }
 };
 
-// o (unscaled) and the sums of a lane's row to their places: o / l and lse, or the parts of a split
-template <int D>
-__device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, int64_t token, const f32x16 (&o)[D / 32], float base,
-                                       float l) {
+// Where a lane's row goes: o / l and lse, or, of a split, o as it is and its sums.  `part` says what of
+// o: part(row, scale) with a row of bf16 or of floats.
+template <typename F>
+__device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, int64_t token, float base, float l,
+                                       bool sums, F &&part) {
   const int64_t at_row = head * A.tq + token;
-  const bool first = (threadIdx.x & 63) < 32;
+  sums = sums && (threadIdx.x & 63) < 32;
   if (A.splits > 1) {
     const int64_t p = int64_t(split) * A.heads * A.tq + at_row;
-    if (first) {
+    if (sums) {
       A.pml[2 * p] = base;
       A.pml[2 * p + 1] = l;
     }
-    store_part<D>(A.po + p * A.dim, o, 1.f, A.dim);
+    part(A.po + p * A.dim, 1.f);
     return;
   }
-  if (first) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
-  store_row<D>(A.o + token * A.ldo + head * A.hso, o, l == 0.f ? 0.f : 1.f / l, A.dim);
+  if (sums) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
+  part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : 1.f / l);
 }
 
 // Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
@@ -185,7 +186,10 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   if (n > 0 && special)
     add_special<D>(o, vp, A.ldv, A.dim, (begin + full) * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
 
-  if (y.valid) finish<D>(A, b.split, y.head, y.sq.q0 + y.token, o, z.base, halves_add(z.l));
+  const float l = halves_add(z.l);
+  if (y.valid)
+    finish(A, b.split, y.head, y.sq.q0 + y.token, z.base, l, true,
+           [&](auto *row, float scale) { store_row(row, o, scale, A.dim); });
 }
 
 // Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
@@ -268,40 +272,48 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
       add_special<D>(o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
                      [&](int j) { return j < y.lim; });
 
-  // the wavefronts' sums by their largest base, one wavefront's o (fp32, [D][32]) in each
-  // half of two of the tiles
+  // The wavefronts' sums by their largest base: o (fp32, four values of a lane a place) goes through
+  // two of the tiles, and each wavefront adds up, and stores, 32 columns.
   __shared__ float bases[4][32], ls[4][32];
   tile_barrier();
-  float *const mine = reinterpret_cast<float *>(wave < 2 ? kt0 : vt0) + (wave & 1) * D * 32;
+  auto place = [&](int w, int t, int b) {
+    return reinterpret_cast<float4 *>(w < 2 ? kt0 : vt0) + (((w & 1) * T + t) * 4 + b) * 64 + lane;
+  };
 #pragma unroll
   for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) mine[(32 * t + d_row(i)) * 32 + (lane & 31)] = o[t][i];
+    for (int b = 0; b < 4; ++b)
+      *place(wave, t, b) = make_float4(o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]);
   const float l = halves_add(z.l);
   if (lane < 32) {
     bases[wave][lane] = z.base;
     ls[wave][lane] = l;
   }
   __syncthreads();
-  if (wave) return;
+  if (wave >= T) return;
   float base = bases[0][lane & 31], sum = 0.f, f[4];
 #pragma unroll
   for (int w = 1; w < 4; ++w) base = fmaxf(base, bases[w][lane & 31]);
+  f32x16 out;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) out[i] = 0.f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
+    // a wavefront without keys has a factor of 0 and nothing but zeros
     f[w] = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
     sum += ls[w][lane & 31] * f[w];
-  }
 #pragma unroll
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int e = (32 * t + d_row(i)) * 32 + (lane & 31);
-      const float *const k = reinterpret_cast<const float *>(kt0) + e, *const v = reinterpret_cast<const float *>(vt0) + e;
-      // a wavefront without keys has a factor of 0 and nothing but zeros
-      o[t][i] = k[0] * f[0] + k[D * 32] * f[1] + v[0] * f[2] + v[D * 32] * f[3];
+    for (int b = 0; b < 4; ++b) {
+      const float4 v = *place(w, wave, b);
+      out[4 * b] = fmaf(v.x, f[w], out[4 * b]);
+      out[4 * b + 1] = fmaf(v.y, f[w], out[4 * b + 1]);
+      out[4 * b + 2] = fmaf(v.z, f[w], out[4 * b + 2]);
+      out[4 * b + 3] = fmaf(v.w, f[w], out[4 * b + 3]);
     }
-  if (y.valid) finish<D>(A, b.split, y.head, y.sq.q0 + y.token, o, base, sum);
+  }
+  if (y.valid)
+    finish(A, b.split, y.head, y.sq.q0 + y.token, base, sum, wave == 0,
+           [&](auto *row, float scale) { store_tile(row, out, wave, scale, A.dim); });
 }
 
 // a row's splits joined: sixteen lanes a row, eight columns each
