@@ -803,8 +803,8 @@ int op_dropout(int64_t rows, int64_t cols, int32_t xtype, const void *x, int64_t
  * for each qgroup columns of a row (a power of two from 8 to 512, the last group
  * of a row may be shorter; 0: one for the row).
  * Row strides in elements, 0 for c: ldx of x; ldh of h and res; ldy; ldg; ldd
- * of d and gh.  Elements between the rows are neither read nor written.
- * Widths, strides and addresses are free; c <= 32768, rows < 2^31.
+ * of d and gh.  What lies between the rows is not written, and not used.
+ * Widths, strides and addresses are free; c <= 16384, rows < 2^31.
  */
 typedef struct ckpt_rms_desc {
   int64_t rows;
@@ -833,8 +833,8 @@ int op_rms_forward(const ckpt_rms_desc *desc, const void *x, const void *res, co
 int op_rms_apply(const ckpt_rms_desc *desc, const void *h, const float *st, const float *w, void *y,
                  float *ys, void *stream);
 
-/* op_rms_workspace_bytes -- device workspace of op_rms_backward (at most 512 c
- * floats, and 16 bytes more for each 4 that do not divide c). */
+/* op_rms_workspace_bytes -- device workspace of op_rms_backward: a row of floats, its
+ * length rounded up to a multiple of 4, for each workgroup (at most 1536, 17 MB in all). */
 int op_rms_workspace_bytes(const ckpt_rms_desc *desc, uint64_t *bytes);
 
 /*

@@ -53,7 +53,7 @@ Rms rms_of(const ckpt_rms_desc *d, const char *fn) {
   need_ptr(d, fn, "desc");
   if (d->rows < 1 || d->c < 1) refuse(CKPT_E_INVALID, fn, ": rows and c must be positive");
   if (d->rows >= kRows) refuse(CKPT_E_UNSUPPORTED, fn, ": rows must stay below 2^31");
-  if (d->c > 32768) refuse(CKPT_E_UNSUPPORTED, fn, ": c must not exceed 32768");
+  if (d->c > 16384) refuse(CKPT_E_UNSUPPORTED, fn, ": c must not exceed 16384");
   for (int32_t t : {d->xtype, d->htype, d->gtype, d->dtype}) need_type(t, fn);
   need_type(d->ytype, fn, true);
   if (!(d->eps > 0.f) || !std::isfinite(d->eps)) refuse(CKPT_E_INVALID, fn, ": eps must be positive");

@@ -2,11 +2,15 @@
 // st = 1 / sqrt(mean h^2 + eps), y = h st w in 32, 16 or 8 bits; the re-run from kept h
 // and st; the backward d = gh + st (g w - xhat mean(g w xhat)), dw = sum g xhat.
 //
-// One pass: a team (a wavefront for rows of up to 2048 columns, else a workgroup)
+// One pass: a team (a wavefront for rows of up to 1024 columns, else a workgroup)
 // holds a whole row in registers, so every tensor is read or written once.  Teams loop
 // over rows with the weight kept in registers.  A thread's vectors are eight columns
-// each, `TEAM` vectors apart, so a wavefront's accesses are contiguous; the last vector
-// of a row whose width 8 does not divide goes element by element.
+// each, `TEAM` vectors apart, so a wavefront's accesses are contiguous.  The last vector
+// of a row whose width 8 does not divide is loaded whole, into the next row, where there
+// is one, and stored element by element.
+//
+// Bound by HBM (a copy of 256 MiB reaches 5.5 TB/s): 16384 x 4096 with a residual and an 8-bit output
+// 91 us (5.2 TB/s), 16384 x 2048 backward 59 us (4.5 TB/s; its records of sums are 5% more).
 #include "common.h"
 #include "lanes.h"
 #include "seq.h"
@@ -19,13 +23,13 @@ struct E4m3 {
   uint8_t bits;
 };
 
-// eight elements from p, or the first cnt of them (the others 0)
+// eight elements from p, or the first cnt of them (the others 0); over: all eight can be read
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, int cnt, float v[8]) {
-  if (cnt >= 8) {
+__device__ __forceinline__ void load8(const T *p, int cnt, float v[8], bool over = false) {
+  if (cnt >= 8 || over) {
     const Vec<T, 8> r = load_vec<T, 8>(p);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = float(r.v[k]);
+    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? float(r.v[k]) : 0.f;
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = k < cnt ? float(p[k]) : 0.f;
@@ -146,20 +150,22 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_rms_fwd(RmsArgs A) {
   int slot = 0;
   for (int64_t row = blockIdx.x * int64_t(TEAMS) + threadIdx.x / TEAM; row < A.rows;
        row += int64_t(gridDim.x) * TEAMS, slot ^= 1) {
+    const bool more = row + 1 < A.rows && A.c >= 8;
     float v[NV][8];
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[j][k] = 0.f;
-      if (cnt[j] > 0) load8(static_cast<const XT *>(A.x) + row * (APPLY ? A.ldh : A.ldx) + (j * TEAM + t) * 8, cnt[j], v[j]);
+      if (cnt[j] > 0)
+        load8(static_cast<const XT *>(A.x) + row * (APPLY ? A.ldh : A.ldx) + (j * TEAM + t) * 8, cnt[j], v[j], more);
     }
     if constexpr (RES) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
         if (cnt[j] > 0) {
           float r[8];
-          load8(static_cast<const HT *>(A.res) + row * A.ldh + (j * TEAM + t) * 8, cnt[j], r);
+          load8(static_cast<const HT *>(A.res) + row * A.ldh + (j * TEAM + t) * 8, cnt[j], r, more);
           // the norm is of the sum as the stream keeps it
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[j][k] = float((HT)(v[j][k] + r[k]));
@@ -244,6 +250,7 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_rms_bwd(RmsBwdArgs A) {
   int slot = 0;
   for (int64_t row = blockIdx.x * int64_t(TEAMS) + threadIdx.x / TEAM; row < A.rows;
        row += int64_t(gridDim.x) * TEAMS, slot ^= 1) {
+    const bool more = row + 1 < A.rows && A.c >= 8;
     float x[NV][8], g[NV][8], e[NV][8];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -251,9 +258,9 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_rms_bwd(RmsBwdArgs A) {
       for (int k = 0; k < 8; ++k) x[j][k] = g[j][k] = e[j][k] = 0.f;
       const int64_t col = (j * TEAM + t) * 8;
       if (cnt[j] > 0) {
-        load8(static_cast<const HT *>(A.h) + row * A.ldh + col, cnt[j], x[j]);
-        load8(static_cast<const GT *>(A.g) + row * A.ldg + col, cnt[j], g[j]);
-        if (A.gh) load8(static_cast<const DT *>(A.gh) + row * A.ldd + col, cnt[j], e[j]);
+        load8(static_cast<const HT *>(A.h) + row * A.ldh + col, cnt[j], x[j], more);
+        load8(static_cast<const GT *>(A.g) + row * A.ldg + col, cnt[j], g[j], more);
+        if (A.gh) load8(static_cast<const DT *>(A.gh) + row * A.ldd + col, cnt[j], e[j], more);
       }
     }
     const float st = A.st[row];
@@ -318,7 +325,9 @@ __global__ __launch_bounds__(1024) void k_rms_dw(const float *part, int groups, 
   }
 }
 
-// a row's team and vectors a thread: a wavefront where four vectors a thread hold the row
+// A row's team and vectors a thread.  At 134 MB a tensor of 16 bits: rows of 2048 by a wavefront with
+// four vectors a thread 55 us forward and 79 backward, by a workgroup with one 51 and 58; rows of
+// 8192 by 256 threads with four 54 and 84, by 1024 with one 49 and 61.
 template <typename F>
 void with_team(int c, F &&f) {
   using std::integral_constant;
@@ -326,11 +335,10 @@ void with_team(int c, F &&f) {
 #define CKPT_TEAM(team, nv) f(integral_constant<int, team>(), integral_constant<int, nv>())
   if (vecs <= 64) CKPT_TEAM(64, 1);
   else if (vecs <= 128) CKPT_TEAM(64, 2);
-  else if (vecs <= 256) CKPT_TEAM(64, 4);
+  else if (vecs <= 256) CKPT_TEAM(256, 1);
   else if (vecs <= 512) CKPT_TEAM(256, 2);
-  else if (vecs <= 1024) CKPT_TEAM(256, 4);
-  else if (vecs <= 2048) CKPT_TEAM(1024, 2);
-  else CKPT_TEAM(1024, 4);
+  else if (vecs <= 1024) CKPT_TEAM(1024, 1);
+  else CKPT_TEAM(1024, 2);
 #undef CKPT_TEAM
 }
 
@@ -339,7 +347,8 @@ void launch_fwd(hipStream_t s, const RmsArgs &a) {
   with_team(a.c, [&](auto team, auto nv) {
     constexpr int TEAM = team, NV = nv, TEAMS = block_of(TEAM) / TEAM;
     const int64_t need = (int64_t(a.rows) + TEAMS - 1) / TEAMS;
-    const int64_t fill = 256 * 2048 / block_of(TEAM);
+    // a few rows each: 16384 x 4096 with an 8-bit output 92 us, with four times as many each 102
+    const int64_t fill = 1024 * 2048 / block_of(TEAM);
     hipLaunchKernelGGL((k_rms_fwd<XT, HT, YT, RES, APPLY, TEAM, NV>), dim3(uint32_t(need < fill ? need : fill)),
                        dim3(block_of(TEAM)), 0, s, a);
   });
@@ -380,11 +389,18 @@ void rms_forward(hipStream_t s, const RmsArgs &a, int xtype, int htype, int ytyp
     hf ? forward_y<__bf16, float, true, false>(s, a, ytype) : forward_y<__bf16, __bf16, true, false>(s, a, ytype);
 }
 
-// workgroups of a backward: two for each compute unit, each with a record of c sums
+// Workgroups of a backward, each with a record of c sums: as many as are resident together, for with
+// fewer the loads in flight do not cover the memory's latency, and a second round of workgroups finds
+// them all at the same place again (16384 x 2048: 512 take 79 us, 1024 64, 1536 60, 2048 73).
 int rms_backward_groups(int64_t rows, int c) {
-  const int teams = c <= 2048 ? 4 : 1;
+  int most = 0, teams = 0;
+  with_team(c, [&](auto team, auto nv) {
+    constexpr int TEAM = team, NV = nv;
+    teams = block_of(TEAM) / TEAM;
+    most = TEAM == 1024 ? (NV == 1 ? 512 : 256) : NV == 1 ? 1536 : 1024;
+  });
   const int64_t need = (rows + teams - 1) / teams;
-  return int(need < 512 ? need : 512);
+  return int(need < most ? need : most);
 }
 
 void rms_backward(hipStream_t s, const RmsBwdArgs &a, int groups, int gtype, int htype, int dtype) {

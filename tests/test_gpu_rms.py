@@ -2,8 +2,8 @@
 
 Bars, per element: half a step of the output's type for the rounding at the end, plus
 L 2^-24 times the magnitudes that enter it for the fp32 arithmetic.  A row's sum
-runs over at most 32 values in a thread and trees of 64 lanes and 16 wavefronts (below
-32 + 6 + 16 operations), a column's over at most 40 rows here in a team, 4 teams, 32
+runs over at most 16 values in a thread and trees of 64 lanes and 16 wavefronts (below
+16 + 6 + 16 operations), a column's over at most 40 rows here in a team, 4 teams, 32
 records and 16 wavefronts; the few operations before and after are covered by the distance to 256.
 """
 import numpy as np
@@ -18,7 +18,7 @@ torch = pytest.importorskip("torch")
 L = 256 * 2.0 ** -24
 EPS = 1e-5
 # widths of every team and vector count, full and not, and odd ones
-WIDTHS = [1, 7, 8, 64, 333, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4096, 4100, 8192, 8200, 16384, 16391, 32768]
+WIDTHS = [1, 7, 8, 64, 333, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4096, 4100, 8192, 8200, 16381, 16384]
 
 
 class Case:
@@ -129,7 +129,7 @@ def test_row_counts(rows):
     t.check_backward()
 
 
-@pytest.mark.parametrize("y,group,c", [("bf16", 0, 1000), ("f8", 128, 1024), ("f8", 0, 4104), ("f32", 0, 20000)])
+@pytest.mark.parametrize("y,group,c", [("bf16", 0, 1000), ("f8", 128, 1024), ("f8", 0, 4104), ("f32", 0, 12000)])
 def test_rerun_gives_the_same_bits(y, group, c):
     t = Case(21, c, y=y, group=group)
     t.forward()
