@@ -5,7 +5,7 @@
 //   k_embed_sort  orders the tokens by id, each id's in their order.  A workgroup
 //     takes a range of ids, reads all ids (from L2: they are few against the rows),
 //     counts those of its range for each of sixteen sections of the tokens, one a
-//     wavefront, and places them.  The first position of a range is the number of
+//     wavefront, lists them, and places them.  The first position of a range is the number of
 //     smaller ids, which the workgroup counts as it goes, so workgroups need nothing of
 //     each other.
 //   k_embed_sum   a wavefront takes a chunk of sorted positions, 512 columns, and adds up
@@ -26,6 +26,7 @@ namespace ckpt {
 namespace {
 
 constexpr int SECTIONS = 16;    // wavefronts of a sorting workgroup
+constexpr int LIST = 512;       // tokens of a section that are kept from the first reading
 constexpr int MAX_RANGE = 1024; // ids of one: [SECTIONS][MAX_RANGE] counts take 64 KB of LDS
 
 template <typename T>
@@ -122,6 +123,7 @@ template <bool WIDE>
 __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int range) {
   __shared__ int cnt[SECTIONS * MAX_RANGE];  // [section][id of the range]
   __shared__ int wsum[SECTIONS];
+  __shared__ unsigned lists[SECTIONS][LIST];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lo = int(min(int64_t(blockIdx.x) * range, A.vocab));
   const int n = int(min(int64_t(range), A.vocab - lo));
@@ -130,18 +132,32 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   for (int i = threadIdx.x; i < SECTIONS * range; i += 64 * SECTIONS) cnt[i] = 0;
   __syncthreads();
 
-  int less = 0;
-  each_ids<WIDE>(A, first, last, [&](int64_t, const int (&id)[4]) {
+  // the range's tokens go to the wavefront's list as they are met, in order
+  unsigned *const list = lists[wave];
+  int less = 0, listed = 0;
+  each_ids<WIDE>(A, first, last, [&](int64_t i, const int (&id)[4]) {
+    bool in[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) less += unsigned(id[u]) < unsigned(lo);
-    unsigned nearest = ~0u;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) nearest = min(nearest, unsigned(id[u]) - unsigned(lo));
-    if (nearest < unsigned(n)) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (unsigned(id[u]) - unsigned(lo) < unsigned(n)) atomicAdd(&cnt[wave * range + id[u] - lo], 1);
+    for (int u = 0; u < 4; ++u) {
+      less += unsigned(id[u]) < unsigned(lo);
+      in[u] = unsigned(id[u]) - unsigned(lo) < unsigned(n);
     }
+    if (!__any(in[0] | in[1] | in[2] | in[3])) return;
+    uint64_t m[4];
+    int at = listed;  // of the lane's first
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      m[u] = __ballot(in[u]);
+      at += __popcll(m[u] & ((1ull << lane) - 1));
+      listed += __popcll(m[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (in[u]) {
+        atomicAdd(&cnt[wave * range + id[u] - lo], 1);
+        if (at < LIST) list[at] = unsigned(i - first + lane * 4 + u) | unsigned(id[u] - lo) << 22;
+        ++at;
+      }
   });
 #pragma unroll
   for (int o = 32; o; o >>= 1) less += __shfl_xor(less, o);
@@ -188,6 +204,27 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   }
   __syncthreads();
 
+  if (listed <= LIST && per <= (1 << 22)) {
+    for (int i = 0; i < listed; i += 64) {
+      const int m = min(64, listed - i);
+      const unsigned entry = lane < m ? list[i + lane] : ~0u;
+      const int id = int(entry >> 22);
+      int rank = lane;  // tokens of the same id before the lane's, of these 64
+      if (__any(lane < m && id != __builtin_amdgcn_readfirstlane(id))) {
+        rank = 0;
+        for (int j = 0; j + 1 < m; ++j) rank += lane > j && __builtin_amdgcn_readlane(id, j) == id;
+      }
+      if (lane < m) {
+        int *const at = &cnt[wave * range + id];
+        const int p = *static_cast<volatile int *>(at) + rank;
+        A.perm[p] = int(first) + int(entry & ((1u << 22) - 1));
+        A.key[p] = lo + id;
+        atomicAdd(at, 1);  // the wavefront's reads above come first
+      }
+    }
+    return;
+  }
+  // a longer list, or a section that 22 bits do not number, is read again
   each_ids<WIDE>(A, first, last, [&](int64_t i, const int (&id)[4]) {
     bool in[4];
 #pragma unroll
@@ -293,7 +330,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int z
     for (int u = 0; u < 8; ++u) {
       const int64_t row = token_at(min(q + u, q1 - 1));
       const GT *const p = static_cast<const GT *>(A.src) + row * A.lds + col;
-      if (cnt >= 8) {
+      if (cnt >= 8 || (row + 1 < A.tokens && A.c >= 8)) {  // past an odd row's end lies the next row
         v[u] = load_vec<GT, 8>(p);
       } else {
 #pragma unroll
