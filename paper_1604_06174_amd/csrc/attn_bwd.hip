@@ -27,6 +27,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
   const int token = int(r / A.rep), head = kvh * A.rep + int(r - int64_t(token) * A.rep);
   const int past = sq.lk - sq.lq;
   const int lim = A.causal ? min(sq.lk, max(0, token + past + 1)) : sq.lk;
+  const int lim_hi = __builtin_amdgcn_readlane(lim, 31);  // the wavefront's most
   const int lim_lo = A.causal ? min(sq.lk, max(0, int(sq.first / A.rep) + past + 1)) : sq.lk;  // the workgroup's least
   const int64_t last = min(sq.first + BM, rows) - 1;
   const int kend = A.causal ? min(sq.lk, max(0, int(last / A.rep) + past + 1)) : sq.lk;
@@ -79,6 +80,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
     const int left = lim - it * BN - 4 * (lane >> 5);  // keys the lane's query sees from its half's first on
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
+      if (MASKED && it * BN + u * 32 >= lim_hi) break;  // nothing for the wavefront's rows
       f32x16 s[1], dp[1];
       clear(s);
       clear(dp);
@@ -134,6 +136,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {
   const int past = sq.lk - sq.lq;
   // the first query that sees the key, and the workgroup's first tile
   const int from = A.causal ? max(0, key - past) : 0;
+  const int from_lo = __builtin_amdgcn_readfirstlane(from);  // the wavefront's least
   const int begin = (A.causal ? max(0, first - past) : 0) / BN, end = (sq.lq + BN - 1) / BN;
   const int heads = A.rep / A.parts, head0 = kvh * A.rep + part * heads;
   const int per = max(0, end - begin), n = per * heads;  // tiles of a head, of all
@@ -180,6 +183,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {
     const int unseen = from - t0 - 4 * (lane >> 5);  // queries that do not see the lane's key, from its half's first on
 #pragma unroll
     for (int u = 0; u < BN / 32; ++u) {
+      if (MASKED && t0 + u * 32 + 32 <= from_lo) continue;  // no query that sees the wavefront's keys
       f32x16 s[1], dp[1];
       clear(s);
       clear(dp);

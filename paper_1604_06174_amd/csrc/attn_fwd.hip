@@ -105,47 +105,29 @@ __device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, i
   part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : 1.f / l);
 }
 
-// Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
-// joined at the end.
+// A wavefront's 32 rows as 32 keys after the other go by.
 template <int D>
-__global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
-  constexpr int BM = 128, BN = 32, T = D / 32, KK = D / 16;
-  __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Block b(A);
-  Query<BM> y;
-  if (!y.find(A, tiles, b.tile, b.kvh, wave * 32 + (lane & 31))) return;
-  const int lk = y.sq.lk;
-  int begin, end;
-  b.share(A, (y.kend + BN - 1) / BN, begin, end);
-  const int n = end - begin;
-
+struct Rows {
+  static constexpr int T = D / 32, KK = D / 16;
   bf16x8 q[KK];
-  {
-    const __bf16 *p = A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
-  }
-  const Places<D> places;
-  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
-  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
-
   f32x16 o[T];
-  clear(o);
-  Sums z(A.scale * LOG2E);
-  __shared__ int special;
-  if (threadIdx.x == 0) special = 0;
+  Sums z;
 
-  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    const Places<D> at = places.here();
+  __device__ __forceinline__ Rows(const AttnArgs &A, const __bf16 *query) : z(A.scale * LOG2E) {
 #pragma unroll
-    for (int sub = 0; sub < BN / 32; ++sub) {
-    const int left = y.lim - (it * BN + sub * 32) - 4 * (lane >> 5);  // keys the row sees from its half's first on
+    for (int kk = 0; kk < KK; ++kk) q[kk] = kept(query, kk, A.dim);
+    clear(o);
+  }
+  // the 32 keys and values from row `first` of the tiles on; `seen`: how many of them the lane's row sees
+  // (MASKED: it may be less than all)
+  template <bool MASKED>
+  __device__ __forceinline__ void turn(const Places<D> &at, const unsigned char *kt, const unsigned char *vt, int first,
+                                       int seen) {
     f32x16 s[1];
     clear(s);
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) s[0] = mfma(at.rows(kt, sub * 32, kk), q[kk], s[0]);
+    for (int kk = 0; kk < KK; ++kk) s[0] = mfma(at.rows(kt, first, kk), q[kk], s[0]);
+    const int left = seen - 4 * ((threadIdx.x & 63) >> 5);  // from the first key of the lane's half on
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -165,14 +147,23 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
       z.l += s[0][i];
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, sub * 32 + 16 * c, operand(s[0], c));
-    }
-  };
-  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;  // tiles that every row sees whole
+    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, first + 16 * c, operand(s[0], c));
+  }
+};
+
+// The loop over tiles [begin, end) of BN keys that both kernels share: work(tile, kt, vt, masked) on each,
+// the next loading meanwhile.  Tiles that not every row sees whole have their values scrubbed; the first
+// of them is returned.
+template <int D, int BN, typename F>
+__device__ __forceinline__ int each_tile(const Loader<D, BN, 256> &kload, const Loader<D, BN, 256> &vload, int begin,
+                                         int end, int lim_lo, int lk, unsigned char *kt0, unsigned char *kt1,
+                                         unsigned char *vt0, unsigned char *vt1, int &special, F &&work) {
   auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
     kload.load(kt, int64_t(it) * BN, lk - it * BN);
     vload.load(vt, int64_t(it) * BN, lk - it * BN);
   };
+  const int n = end - begin, full = max(0, min(n, lim_lo / BN - begin)) & ~1;
+  if (threadIdx.x == 0) special = 0;
   if (n > 0) load(begin, kt0, vt0);
   two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
     tile_barrier();
@@ -183,21 +174,54 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
     if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
     work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
-  if (n > 0 && special)
-    add_special<D>(o, vp, A.ldv, A.dim, (begin + full) * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
+  return begin + full;
+}
 
-  const float l = halves_add(z.l);
+// Four wavefronts of 32 rows share tiles of 32 keys, which leaves room for three of them on each SIMD.
+// Bound by the vector and matrix units together, and by power (16384 tokens, 16/4 heads of 128 in seven
+// sequences: 226 us, 894 TFLOP/s of the visible products, at 2.0 GHz; the library's largest bf16 products
+// reach 1300).  Tiles of 64 keys with two wavefronts took 4% longer, and so did the scores, exponentials
+// and values of three turns side by side; 64 rows a wavefront, one a SIMD, 25%.
+template <int D>
+__global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
+  constexpr int BM = 128, BN = 32;
+  __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
+  __shared__ int special;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Block b(A);
+  Query<BM> y;
+  if (!y.find(A, tiles, b.tile, b.kvh, wave * 32 + (lane & 31))) return;
+  const int lk = y.sq.lk, lim_hi = __builtin_amdgcn_readlane(y.lim, 31);  // the wavefront's most
+  int begin, end;
+  b.share(A, (y.kend + BN - 1) / BN, begin, end);
+
+  Rows<D> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
+  const Places<D> places;
+  const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
+  const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
+  const int scrubbed =
+      each_tile(kload, vload, begin, end, y.lim_lo, lk, kt0, kt1, vt0, vt1, special,
+                [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
+                  constexpr bool MASKED = decltype(masked)::value;
+                  if (MASKED && it * BN >= lim_hi) return;  // nothing for the wavefront's rows
+                  r.template turn<MASKED>(places.here(), kt, vt, 0, y.lim - it * BN);
+                });
+  if (begin < end && special)
+    add_special<D>(r.o, vp, A.ldv, A.dim, scrubbed * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
+  const float l = halves_add(r.z.l);
   if (y.valid)
-    finish(A, b.split, y.head, y.sq.q0 + y.token, z.base, l, true,
-           [&](auto *row, float scale) { store_row(row, o, scale, A.dim); });
+    finish(A, b.split, y.head, y.sq.q0 + y.token, r.z.base, l, true,
+           [&](auto *row, float scale) { store_row(row, r.o, scale, A.dim); });
 }
 
 // Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
-// joined at the end.
+// joined at the end.  Bound by HBM, with about 7 us of a workgroup's own at its start and end (16 single
+// tokens, 32/8 heads of 128, up to 8192 keys: 75 us, 4.0 TB/s; all of 4096 keys 5.0 TB/s).
 template <int D>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
-  constexpr int BM = 32, BN = 128, T = D / 32, KK = D / 16;
+  constexpr int BM = 32, BN = 128, T = D / 32;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
+  __shared__ int special;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Block b(A);
   Query<BM> y;
@@ -205,93 +229,41 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   const int lk = y.sq.lk;
   int begin, end;
   b.share(A, (y.kend + BN - 1) / BN, begin, end);
-  const int n = end - begin;
 
-  bf16x8 q[KK];
-  {
-    const __bf16 *p = A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = kept(p, kk, A.dim);
-  }
+  Rows<D> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
   const Places<D> places;
   const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
   const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
-
-  f32x16 o[T];
-  clear(o);
-  Sums z(A.scale * LOG2E);
-  __shared__ int special;
-  if (threadIdx.x == 0) special = 0;
-
-  auto work = [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    const Places<D> at = places.here();
-    const int left = y.lim - (it * BN + wave * 32) - 4 * (lane >> 5);  // keys the row sees from its half's first on
-    f32x16 s[1];
-    clear(s);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) s[0] = mfma(at.rows(kt, wave * 32, kk), q[kk], s[0]);
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (MASKED && 8 * (i / 4) + i % 4 >= left) s[0][i] = -INFINITY;
-      top = fmaxf(top, s[0][i]);
-    }
-    if (z.rises(halves_max(top))) {
-      const float f = z.move();
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] *= f;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[0][i] = z.exponential(s[0][i]);
-      z.l += s[0][i];
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, wave * 32 + 16 * c, operand(s[0], c));
-  };
-  const int full = max(0, min(n, y.lim_lo / BN - begin)) & ~1;  // tiles that every row sees whole
-  auto load = [&](int it, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
-    kload.load(kt, int64_t(it) * BN, lk - it * BN);
-    vload.load(vt, int64_t(it) * BN, lk - it * BN);
-  };
-  if (n > 0) load(begin, kt0, vt0);
-  two_kinds(n, full, [&](int i, auto place, auto masked) __attribute__((always_inline)) {
-    tile_barrier();
-    if constexpr (decltype(masked)::value) {
-      scrub<BN * D * 2>(place ? vt1 : vt0, special);
-      __syncthreads();
-    }
-    if (i + 1 < n) load(begin + i + 1, place ? kt0 : kt1, place ? vt0 : vt1);
-    work(begin + i, place ? kt1 : kt0, place ? vt1 : vt0, masked);
-  });
-  if (n > 0 && special)
-    for (int it = begin + full; it < end; ++it)
-      add_special<D>(o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
+  const int scrubbed =
+      each_tile(kload, vload, begin, end, y.lim_lo, lk, kt0, kt1, vt0, vt1, special,
+                [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
+                  r.template turn<decltype(masked)::value>(places.here(), kt, vt, wave * 32, y.lim - it * BN - wave * 32);
+                });
+  if (begin < end && special)
+    for (int it = scrubbed; it < end; ++it)
+      add_special<D>(r.o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
                      [&](int j) { return j < y.lim; });
 
   // The wavefronts' sums by their largest base: o (fp32, four values of a lane a place) goes through
   // two of the tiles, and each wavefront adds up, and stores, 32 columns.
   __shared__ float bases[4][32], ls[4][32];
   tile_barrier();
-  auto place = [&](int w, int t, int b) {
-    return reinterpret_cast<float4 *>(w < 2 ? kt0 : vt0) + (((w & 1) * T + t) * 4 + b) * 64 + lane;
+  auto place = [&](int w, int t, int c) {
+    return reinterpret_cast<float4 *>(w < 2 ? kt0 : vt0) + (((w & 1) * T + t) * 4 + c) * 64 + lane;
   };
 #pragma unroll
   for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
-      *place(wave, t, b) = make_float4(o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]);
-  const float l = halves_add(z.l);
+    for (int c = 0; c < 4; ++c)
+      *place(wave, t, c) = make_float4(r.o[t][4 * c], r.o[t][4 * c + 1], r.o[t][4 * c + 2], r.o[t][4 * c + 3]);
+  const float l = halves_add(r.z.l);
   if (lane < 32) {
-    bases[wave][lane] = z.base;
+    bases[wave][lane] = r.z.base;
     ls[wave][lane] = l;
   }
   __syncthreads();
   if (wave >= T) return;
-  float base = bases[0][lane & 31], sum = 0.f, f[4];
+  float base = bases[0][lane & 31], sum = 0.f;
 #pragma unroll
   for (int w = 1; w < 4; ++w) base = fmaxf(base, bases[w][lane & 31]);
   f32x16 out;
@@ -300,15 +272,15 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     // a wavefront without keys has a factor of 0 and nothing but zeros
-    f[w] = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
-    sum += ls[w][lane & 31] * f[w];
+    const float f = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
+    sum += ls[w][lane & 31] * f;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const float4 v = *place(w, wave, b);
-      out[4 * b] = fmaf(v.x, f[w], out[4 * b]);
-      out[4 * b + 1] = fmaf(v.y, f[w], out[4 * b + 1]);
-      out[4 * b + 2] = fmaf(v.z, f[w], out[4 * b + 2]);
-      out[4 * b + 3] = fmaf(v.w, f[w], out[4 * b + 3]);
+    for (int c = 0; c < 4; ++c) {
+      const float4 v = *place(w, wave, c);
+      out[4 * c] = fmaf(v.x, f, out[4 * c]);
+      out[4 * c + 1] = fmaf(v.y, f, out[4 * c + 1]);
+      out[4 * c + 2] = fmaf(v.z, f, out[4 * c + 2]);
+      out[4 * c + 3] = fmaf(v.w, f, out[4 * c + 3]);
     }
   }
   if (y.valid)
