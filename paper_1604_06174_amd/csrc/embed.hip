@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int z
     for (int u = 0; u < 8; ++u) {
       const int64_t row = token_at(min(q + u, q1 - 1));
       const GT *const p = static_cast<const GT *>(A.src) + row * A.lds + col;
-      if (cnt >= 8 || (row + 1 < A.tokens && A.c >= 8)) {  // past an odd row's end lies the next row
+      if (cnt >= 8 || (cnt > 0 && row + 1 < A.tokens && A.c >= 8)) {  // past an odd row's end lies the next row
         v[u] = load_vec<GT, 8>(p);
       } else {
 #pragma unroll
