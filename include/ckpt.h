@@ -855,7 +855,7 @@ int op_rms_backward(const ckpt_rms_desc *desc, const void *g, const void *gh, co
  * gradient.  Strides in elements, 0 for c: ldw of the table and its gradient,
  * ldy, ldg.  accumulate = 1: op_embed_backward adds to the table's gradient
  * (an output layer that shares the table has left its part there).
- * tokens < 2^31, vocab < 2^31, c <= 2^20.
+ * tokens <= 2^30, vocab < 2^31, c <= 2^20, tokens c < 2^36.
  */
 typedef struct ckpt_embed_desc {
   int64_t tokens, vocab;
@@ -896,8 +896,9 @@ int op_embed_backward(const ckpt_embed_desc *desc, const void *ids, const void *
  * scale multiplies the scores (0: 1 / sqrt(dim)).  Elements from row to row ld?
  * (0: heads or kv_heads times dim) and from head to head hs? (0: dim) of q, k, v
  * and o; multiples of 8, addresses of 16 bytes.  g has o's strides; dq, dk and dv
- * those of q, k and v.
- * tq, tk < 2^31, seqs < 2^20, heads <= 4096.
+ * those of q, k and v.  Rows of an output must not overlap.
+ * tq, tk <= 2^30, seqs < 2^20, heads <= 4096, (tq heads + tk kv_heads) / 128 + 2 seqs
+ * kv_heads < 2^24.
  */
 typedef struct ckpt_attn_desc {
   int64_t tq, tk;

@@ -97,7 +97,8 @@ __device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int size, 
     Sequence mine{0, 0, 0, 0, 0};
     if (lane < A.seqs) rows_of(A, lane, mine);
     const int n = int((int64_t(QUERIES ? mine.lq : mine.lk) * per + size - 1) / size);
-    const int low = QUERIES && A.causal ? int(int64_t(max(0, mine.lk - mine.lq)) * per / size) : 0;
+    // (it orders and no more: so long a past that 32 bits do not hold its tiles counts as a shorter one)
+    const int low = QUERIES && A.causal ? int(min(int64_t(max(0, mine.lk - mine.lq)) * per / size, int64_t(1) << 29)) : 0;
     const bool single = !__any(n > 1);  // then a level's tiles are counted without adding up
     auto above = [&](int w) {
       return single ? int(__popcll(__ballot(n > 0 && low >= w))) : wave_add(max(0, min(n, low + n - w)));

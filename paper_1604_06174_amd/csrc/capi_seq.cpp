@@ -100,9 +100,11 @@ ckpt::RmsArgs rms_args(const ckpt_rms_desc *d, const Rms &r, const float *w, voi
 ckpt::EmbedArgs embed_of(const ckpt_embed_desc *d, bool backward, const char *fn) {
   need_ptr(d, fn, "desc");
   if (d->tokens < 1 || d->vocab < 1 || d->c < 1) refuse(CKPT_E_INVALID, fn, ": tokens, vocab and c must be positive");
-  if (d->tokens >= kRows || d->vocab >= kRows) refuse(CKPT_E_UNSUPPORTED, fn, ": tokens and vocab must stay below 2^31");
+  if (d->tokens > kRows / 2) refuse(CKPT_E_UNSUPPORTED, fn, ": tokens must not exceed 2^30");
+  if (d->vocab >= kRows) refuse(CKPT_E_UNSUPPORTED, fn, ": vocab must stay below 2^31");
   if (d->c > (1 << 20)) refuse(CKPT_E_UNSUPPORTED, fn, ": c must not exceed 2^20");
-  if (product(d->tokens, d->c) >= (int64_t(1) << 40)) refuse(CKPT_E_UNSUPPORTED, fn, ": tokens*c must stay below 2^40");
+  // a launch has fewer than 2^32 threads
+  if (product(d->tokens, d->c) >= (int64_t(1) << 36)) refuse(CKPT_E_UNSUPPORTED, fn, ": tokens*c must stay below 2^36");
   for (int32_t t : {d->wtype, d->ytype, d->gtype, d->dtype}) need_type(t, fn);
   if ((d->ids64 != 0 && d->ids64 != 1) || (d->accumulate != 0 && d->accumulate != 1))
     refuse(CKPT_E_INVALID, fn, ": ids64 and accumulate are 0 or 1");
@@ -130,11 +132,12 @@ ckpt::AttnArgs attn_of(const ckpt_attn_desc *d, const char *fn) {
   if (d->dim % 8 || d->dim > 128) refuse(CKPT_E_UNSUPPORTED, fn, ": dim must be a multiple of 8, at most 128");
   if (d->causal != 0 && d->causal != 1) refuse(CKPT_E_INVALID, fn, ": causal is 0 or 1");
   if (!(d->scale >= 0.f) || !std::isfinite(d->scale)) refuse(CKPT_E_INVALID, fn, ": scale must be positive, or 0");
-  if (d->tq >= kRows || d->tk >= kRows) refuse(CKPT_E_UNSUPPORTED, fn, ": tq and tk must stay below 2^31");
+  if (d->tq > kRows / 2 || d->tk > kRows / 2) refuse(CKPT_E_UNSUPPORTED, fn, ": tq and tk must not exceed 2^30");
   if (d->seqs >= (1 << 20) || d->heads > 4096) refuse(CKPT_E_UNSUPPORTED, fn, ": too many sequences or heads");
-  // workgroups: tiles of at least 32 rows, each sequence's last partly filled
-  if ((d->tq / 16 + d->tk / 16 + d->seqs) * d->heads >= (int64_t(1) << 31))
-    refuse(CKPT_E_UNSUPPORTED, fn, ": tensor too large");
+  // workgroups of 256 threads, of which a launch has fewer than 2^32: tiles of 128 rows, or of 32 if
+  // that takes no more than one for each sequence besides its last, partly filled one
+  if ((d->tq * d->heads + d->tk * d->kv_heads) / 128 + 2 * int64_t(d->seqs) * d->kv_heads >= (int64_t(1) << 24))
+    refuse(CKPT_E_UNSUPPORTED, fn, ": more than 2^24 tiles of 128 rows");
   ckpt::AttnArgs a{};
   const int64_t h = d->heads, kv = d->kv_heads, dim = d->dim;
   auto strides = [&](int64_t ld, int64_t hs, int64_t n, int64_t rows, int64_t &lo, int64_t &ho) {

@@ -313,3 +313,29 @@ def test_offsets_past_32_bits():
     wo, wl, eo, el = S.attention(q, kv, kv, np.array([0, 2]), np.array([0, lk]), True, dim ** -0.5)
     close("o", host(o), wo, eo)
     close("lse", host(lse), wl, el)
+
+
+def test_a_past_of_more_tiles_than_32_bits_hold():
+    """Four single tokens of 128 heads on one key head, one of them behind 2^29 keys: one key has a
+    score of 40 and the others of 0, so the answer is its value (they add 2^29 exp(-40) < 2^-28 of it)."""
+    n, heads, dim, at = 1 << 29, 128, 8, (1 << 29) - 12345
+    k = torch.zeros(n + 3, 1, dim, dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    k[at], v[at] = 5.0, torch.arange(1.0, dim + 1, device=DEV).to(torch.bfloat16)
+    v[n:] = 3.0
+    q = torch.ones(4, heads, dim, dtype=torch.bfloat16, device=DEV)
+    o, lse = torch.full_like(q, GUARD), torch.full((heads, 4), GUARD, device=DEV)
+    c = K()
+    desc = c.attn_desc(4, n + 3, 4, heads, 1, dim, scale=1.0)
+    off = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    nb = c.op_attn_workspace_bytes(desc, False)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device=DEV)
+    c.op_attn_forward(desc, q, k, v, off(0, 1, 2, 3, 4), off(0, n, n + 1, n + 2, n + 3), o, lse, ws, nb)
+    want = np.full((4, heads, dim), 3.0)
+    want[0] = np.arange(1, dim + 1)
+    # the probability and the output are rounded to bf16, half a step each
+    close("o", host(o), want, (2 * S.U16 + 2.0 ** -20) * want)
+    wl = np.zeros((heads, 4))
+    wl[:, 0] = 40.0
+    # a logarithm of a few operations on numbers up to 40 / ln 2, and 2^-28 of the others
+    close("lse", host(lse), wl, np.where(wl > 0, 64 * 8 * S.U24, 8 * S.U24))

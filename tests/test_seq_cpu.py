@@ -148,7 +148,7 @@ def test_embedding_invalid(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(tokens=1 << 31), dict(vocab=1 << 31), dict(c=(1 << 20) + 1), dict(ldw=1 << 60),
-                                dict(tokens=1 << 25, c=1 << 16)])
+                                dict(tokens=1 << 25, c=1 << 16), dict(tokens=(1 << 30) + 1), dict(tokens=1 << 20, c=1 << 16)])
 def test_embedding_unsupported(kw):
     embed_all(K.E_UNSUPPORTED, **kw)
 
@@ -189,7 +189,8 @@ def test_attention_invalid(kw):
 
 @pytest.mark.parametrize("kw", [dict(dim=12), dict(dim=136), dict(tq=1 << 31), dict(tk=1 << 31), dict(seqs=1 << 20),
                                 dict(heads=8192), dict(ldq=66), dict(hsv=20), dict(ldk=1 << 60),
-                                dict(tq=1 << 30, heads=64)])
+                                dict(tq=1 << 30, heads=64), dict(tq=(1 << 30) + 1, heads=1, kv_heads=1),
+                                dict(tk=1 << 30, seqs=1), dict(seqs=1 << 19, heads=32, kv_heads=32)])
 def test_attention_unsupported(kw):
     attn_all(K.E_UNSUPPORTED, **kw)
 
