@@ -93,7 +93,9 @@ def attention(q, k, v, qoff, koff, causal, scale):
             # a score is off by dim products and sums and a few operations more, its exponential
             # (a power of two, in hardware to about 2^-22) by as much of itself; a sum of lk terms
             rel = (dim + 16) * U24 * 2 * (mag.max(1) + np.abs(base[:, 0])) + (lk + 64) * U24
-            eo[a:b, h] = (U16 + 2 * rel)[:, None] * (p @ np.abs(Vf)) + U16 * np.abs(o[a:b, h]) + 1e-30
+            # o is the mean of the values by the rounded weights, so with weights off by u p at most it is off by
+            # sum u p |v - o| <= u (sum p |v| + |o|), and rounded itself
+            eo[a:b, h] = (U16 + 2 * rel)[:, None] * (p @ np.abs(Vf)) + 2 * U16 * np.abs(o[a:b, h]) + 1e-30
             el[h, a:b] = np.where(none, 0, rel + 4 * U24 * np.abs(np.where(none, 0, lse[h, a:b])))
     return o, lse, eo, el
 

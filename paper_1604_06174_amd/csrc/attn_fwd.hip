@@ -18,10 +18,12 @@ using namespace at;
 // A row's softmax as it goes on: exponentials are powers of two relative to `base`, and l is their
 // sum.  The base is a whole number, so that moving it scales by a power of two, which rounds
 // nothing; it is moved only when an exponential would exceed 2^8, which keeps the sums far inside
-// fp32.
+// fp32.  The products with the values take the exponentials rounded to bf16, so o is divided by the sum of
+// these, lr: it is a mean of the values by weights that add up to 1, exact where a row sees one key
+// (with l it would be off by half a step of bf16), and lse takes l.
 struct Sums {
   float sc;  // of scores to exponents
-  float base = -INFINITY, l = 0.f, top = 0.f;
+  float base = -INFINITY, l = 0.f, lr = 0.f, top = 0.f;
 
   __device__ __forceinline__ explicit Sums(float scale) : sc(scale) {}
   // does a row of the wavefront have to move its base for scores up to `score`?
@@ -35,10 +37,24 @@ struct Sums {
     const float f = to == base ? 1.f : exp2_fast(base - to);
     base = to;
     l *= f;
+    lr *= f;
     return f;
   }
   __device__ __forceinline__ float exponential(float score) const {
     return exp2_fast(fmaf(score, sc, base == -INFINITY ? 0.f : -base));
+  }
+  // to lr: eight rounded exponentials
+  __device__ __forceinline__ void add_rounded(bf16x8 p) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) lr = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[e], p[e + 1]}, ones, lr, false);
+  }
+  // after the last key: l of the whole row, and the factor of o that goes with it
+  __device__ __forceinline__ float end() {
+    l = halves_add(l);
+    lr = halves_add(lr);
+    return l == 0.f ? 0.f : l / lr;
   }
 };
 
@@ -85,11 +101,11 @@ struct Block {
   }
 };
 
-// Where a lane's row goes: o / l and lse, or, of a split, o as it is and its sums.  `part` says what of
+// Where a lane's row goes: factor o / l and lse, or, of a split, factor o and its sums.  `part` says what of
 // o: part(row, scale) with a row of bf16 or of floats.
 template <typename F>
 __device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, int64_t token, float base, float l,
-                                       bool sums, F &&part) {
+                                       float factor, bool sums, F &&part) {
   const int64_t at_row = head * A.tq + token;
   sums = sums && (threadIdx.x & 63) < 32;
   if (A.splits > 1) {
@@ -98,11 +114,11 @@ __device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, i
       A.pml[2 * p] = base;
       A.pml[2 * p + 1] = l;
     }
-    part(A.po + p * A.dim, 1.f);
+    part(A.po + p * A.dim, factor);
     return;
   }
   if (sums) A.lse[at_row] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
-  part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : 1.f / l);
+  part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : factor / l);
 }
 
 // A wavefront's 32 rows as 32 keys after the other go by.
@@ -147,7 +163,11 @@ struct Rows {
       z.l += s[0][i];
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) add_rows<D>(o, at, vt, first + 16 * c, operand(s[0], c));
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8 p = operand(s[0], c);
+      z.add_rounded(p);
+      add_rows<D>(o, at, vt, first + 16 * c, p);
+    }
   }
 };
 
@@ -208,9 +228,9 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
                 });
   if (begin < end && special)
     add_special<D>(r.o, vp, A.ldv, A.dim, scrubbed * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
-  const float l = halves_add(r.z.l);
+  const float factor = r.z.end();
   if (y.valid)
-    finish(A, b.split, y.head, y.sq.q0 + y.token, r.z.base, l, true,
+    finish(A, b.split, y.head, y.sq.q0 + y.token, r.z.base, r.z.l, factor, true,
            [&](auto *row, float scale) { store_row(row, r.o, scale, A.dim); });
 }
 
@@ -246,7 +266,7 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 
   // The wavefronts' sums by their largest base: o (fp32, four values of a lane a place) goes through
   // two of the tiles, and each wavefront adds up, and stores, 32 columns.
-  __shared__ float bases[4][32], ls[4][32];
+  __shared__ float bases[4][32], ls[4][32], factors[4][32];
   tile_barrier();
   auto place = [&](int w, int t, int c) {
     return reinterpret_cast<float4 *>(w < 2 ? kt0 : vt0) + (((w & 1) * T + t) * 4 + c) * 64 + lane;
@@ -256,10 +276,11 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       *place(wave, t, c) = make_float4(r.o[t][4 * c], r.o[t][4 * c + 1], r.o[t][4 * c + 2], r.o[t][4 * c + 3]);
-  const float l = halves_add(r.z.l);
+  const float factor = r.z.end();
   if (lane < 32) {
     bases[wave][lane] = r.z.base;
-    ls[wave][lane] = l;
+    ls[wave][lane] = r.z.l;
+    factors[wave][lane] = factor;
   }
   __syncthreads();
   if (wave >= T) return;
@@ -273,18 +294,19 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   for (int w = 0; w < 4; ++w) {
     // a wavefront without keys has a factor of 0 and nothing but zeros
     const float f = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
+    const float fo = f * factors[w][lane & 31];
     sum += ls[w][lane & 31] * f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const float4 v = *place(w, wave, c);
-      out[4 * c] = fmaf(v.x, f, out[4 * c]);
-      out[4 * c + 1] = fmaf(v.y, f, out[4 * c + 1]);
-      out[4 * c + 2] = fmaf(v.z, f, out[4 * c + 2]);
-      out[4 * c + 3] = fmaf(v.w, f, out[4 * c + 3]);
+      out[4 * c] = fmaf(v.x, fo, out[4 * c]);
+      out[4 * c + 1] = fmaf(v.y, fo, out[4 * c + 1]);
+      out[4 * c + 2] = fmaf(v.z, fo, out[4 * c + 2]);
+      out[4 * c + 3] = fmaf(v.w, fo, out[4 * c + 3]);
     }
   }
   if (y.valid)
-    finish(A, b.split, y.head, y.sq.q0 + y.token, base, sum, wave == 0,
+    finish(A, b.split, y.head, y.sq.q0 + y.token, base, sum, 1.f, wave == 0,
            [&](auto *row, float scale) { store_tile(row, out, wave, scale, A.dim); });
 }
 

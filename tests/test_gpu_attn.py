@@ -315,6 +315,21 @@ def test_offsets_past_32_bits():
     close("lse", host(lse), wl, el)
 
 
+@pytest.mark.parametrize("lens,heads,kv,dim", [(SAME(200, 1, 33, 1, 129), 4, 2, 64), (SAME(1, 1, 2, 1), 8, 2, 128),
+                                               ([(40, 1), (9, 9), (1, 3000)], 2, 2, 40)], ids=["many", "few", "split"])
+def test_a_row_that_sees_one_key_gets_its_value(lens, heads, kv, dim):
+    """Whatever the score and the rounding of its exponential."""
+    t = Case(lens, heads, kv, dim, seed=11, amp=3.0)
+    t.forward()
+    o, n = t.whole(t.d["o"]), 0
+    for a, b, c, d in zip(t.qoff, t.qoff[1:], t.koff, t.koff[1:]):
+        i = a + (b - a) - (d - c)  # the query that sees the first key alone
+        if a <= i < b:
+            assert np.array_equal(o[i], np.repeat(t.v["v"][c], heads // kv, 0))
+            n += 1
+    assert n >= 2
+
+
 def test_a_past_of_more_tiles_than_32_bits_hold():
     """Four single tokens of 128 heads on one key head, one of them behind 2^29 keys: one key has a
     score of 40 and the others of 0, so the answer is its value (they add 2^29 exp(-40) < 2^-28 of it)."""
