@@ -16,6 +16,12 @@
 //   k_embed_join  adds the pieces of such an id, in order.
 // Nothing is added by atomics (the counts are whole numbers), so the same bits come
 // out on every run.
+//
+// Lookups are bound by HBM (32768 rows of 1024 columns, 16 bits: 22 us, 67 MB written and the table's
+// 65 read, 6.1 TB/s with what the caches hold of it).  The gradient of 65536 unevenly distributed tokens, 50000
+// ids, 1024 columns of 16 bits into 32: sort 18 us, bound by its most frequent range (with a loop over the ids in
+// place of the vote on their bits 34), sum 84 (346 MB at 4.1 TB/s, rows in no order), join 12, latency.  The
+// zeros written by the sort's workgroups: sum 62, but sort 17 more and few tokens slower as well.
 #include "common.h"
 #include "seq.h"
 #include "vec.h"
@@ -204,59 +210,42 @@ __global__ __launch_bounds__(64 * SECTIONS) void k_embed_sort(EmbedArgs A, int r
   }
   __syncthreads();
 
+  // 64 tokens in order, a lane each: their places are those of the id's tokens so far and of the lower
+  // lanes with the same id, found by a vote on each bit of the ids
+  const int bits = 32 - __clz(range - 1);
+  auto put = [&](bool in, int id, int token) __attribute__((always_inline)) {
+    uint64_t same = __ballot(in);
+    if (!same) return;
+    for (int k = 0; k < bits; ++k) {
+      const bool one = id >> k & 1;
+      const uint64_t ones = __ballot(one);
+      same &= one ? ones : ~ones;
+    }
+    if (!in) return;
+    // one wavefront's: its accesses are in order, and volatile keeps them in the code's
+    volatile int *const at = &cnt[wave * range + id];
+    const int p = *at + __popcll(same & ((1ull << lane) - 1));
+    A.perm[p] = token;
+    A.key[p] = lo + id;
+    if (same >> lane == 1) *at = p + 1;  // the last of them
+  };
   if (listed <= LIST && per <= (1 << 22)) {
     for (int i = 0; i < listed; i += 64) {
-      const int m = min(64, listed - i);
-      const unsigned entry = lane < m ? list[i + lane] : ~0u;
-      const int id = int(entry >> 22);
-      int rank = lane;  // tokens of the same id before the lane's, of these 64
-      if (__any(lane < m && id != __builtin_amdgcn_readfirstlane(id))) {
-        rank = 0;
-        for (int j = 0; j + 1 < m; ++j) rank += lane > j && __builtin_amdgcn_readlane(id, j) == id;
-      }
-      if (lane < m) {
-        int *const at = &cnt[wave * range + id];
-        const int p = *static_cast<volatile int *>(at) + rank;
-        A.perm[p] = int(first) + int(entry & ((1u << 22) - 1));
-        A.key[p] = lo + id;
-        atomicAdd(at, 1);  // the wavefront's reads above come first
-      }
+      const bool in = i + lane < listed;
+      const unsigned entry = in ? list[i + lane] : 0u;
+      put(in, int(entry >> 22), int(first) + int(entry & ((1u << 22) - 1)));
     }
     return;
   }
   // a longer list, or a section that 22 bits do not number, is read again
-  each_ids<WIDE>(A, first, last, [&](int64_t i, const int (&id)[4]) {
-    bool in[4];
+  for (int64_t i = first; i < last; i += 1024) {
+    int id[16];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) in[u] = unsigned(id[u]) - unsigned(lo) < unsigned(n);
-    // the range's ids of these 256 tokens one after the other, each with all its tokens
-    while (const uint64_t left = __ballot(in[0] | in[1] | in[2] | in[3])) {
-      const int some = in[0] ? id[0] : in[1] ? id[1] : in[2] ? id[2] : id[3];
-      const int key = __builtin_amdgcn_readlane(some, __ffsll((unsigned long long)left) - 1);
-      const uint64_t below = (1ull << lane) - 1;
-      int rank = 0, count = 0;  // the id's tokens in lower lanes, and in all
-      bool same[4];
+    for (int g = 0; g < 16; ++g) id[g] = i + g * 64 + lane < last ? id_at(A, i + g * 64 + lane) : -1;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        same[u] = id[u] == key;
-        const uint64_t b = __ballot(same[u]);
-        rank += __popcll(b & below);
-        count += __popcll(b);
-        in[u] &= !same[u];
-      }
-      // one wavefront's: its accesses are in order, and volatile keeps them in the code's
-      volatile int *const at = &cnt[wave * range + key - lo];
-      int p = *at + rank;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (same[u]) {
-          A.perm[p] = int(i + lane * 4 + u);
-          A.key[p] = key;
-          ++p;
-        }
-      if (lane == 63) *at = p - rank + count - (same[0] + same[1] + same[2] + same[3]);
-    }
-  });
+    for (int g = 0; g < 16; ++g)
+      put(unsigned(id[g]) - unsigned(lo) < unsigned(n), id[g] - lo, int(i) + g * 64 + lane);
+  }
 }
 
 // row `v` of the gradient = the sum, or the sum added to it
