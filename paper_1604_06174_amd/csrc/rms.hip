@@ -10,7 +10,7 @@
 // is one, and stored element by element.
 //
 // Bound by HBM (a copy of 256 MiB reaches 5.5 TB/s): 16384 x 4096 with a residual and an 8-bit output
-// 91 us (5.2 TB/s), 16384 x 2048 backward 59 us (4.5 TB/s; its records of sums are 5% more).
+// 91 us (5.2 TB/s), 16384 x 2048 backward 58 us (4.7 TB/s; its records of sums are 5% more, and their launch 5 us).
 #include "common.h"
 #include "lanes.h"
 #include "seq.h"
@@ -305,22 +305,28 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_rms_bwd(RmsBwdArgs A) {
     if (cnt[j] > 0) store8(A.part + int64_t(blockIdx.x) * A.cpad + (j * TEAM + t) * 8, cnt[j], dw[j]);
 }
 
-// dw = the workgroups' records added up: 64 columns a workgroup, each of sixteen
-// wavefronts every sixteenth record, then the sixteen sums in order
+// dw = the workgroups' records added up: 32 columns a workgroup, each of 32 half wavefronts every 32nd
+// record, sixteen in flight, then the 32 sums in order
 __global__ __launch_bounds__(1024) void k_rms_dw(const float *part, int groups, int c, int cpad, float *dw) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  constexpr int AHEAD = 16;
+  __shared__ float red[32][32];
+  const int lane = threadIdx.x & 31, half = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (col < c) {
-#pragma unroll 8
-    for (int b = wave; b < groups; b += 16) s += part[int64_t(b) * cpad + col];
+    for (int b = half; b < groups; b += 32 * AHEAD) {
+      float v[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) v[u] = part[int64_t(min(b + 32 * u, groups - 1)) * cpad + col];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) s += b + 32 * u < groups ? v[u] : 0.f;
+    }
   }
-  red[wave][lane] = s;
+  red[half][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < c) {
+  if (half == 0 && col < c) {
     float v = red[0][lane];
 #pragma unroll
-    for (int k = 1; k < 16; ++k) v += red[k][lane];
+    for (int k = 1; k < 32; ++k) v += red[k][lane];
     dw[col] = v;
   }
 }
@@ -367,7 +373,7 @@ void launch_bwd(hipStream_t s, const RmsBwdArgs &a, int groups) {
     constexpr int TEAM = team, NV = nv;
     hipLaunchKernelGGL((k_rms_bwd<GT, HT, DT, TEAM, NV>), dim3(groups), dim3(block_of(TEAM)), 0, s, a);
   });
-  hipLaunchKernelGGL(k_rms_dw, dim3((a.c + 63) / 64), dim3(1024), 0, s, a.part, groups, a.c, a.cpad, a.dw);
+  hipLaunchKernelGGL(k_rms_dw, dim3((a.c + 31) / 32), dim3(1024), 0, s, a.part, groups, a.c, a.cpad, a.dw);
 }
 
 template <typename GT, typename HT>
