@@ -844,29 +844,32 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
 
 
 # -------------------------------------------------- units of token models --
-# tensors by type code; an 8-bit output may also be given as plain bytes
-_SEQ_DTYPES = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+# tensors by type code (an unknown one is the library's to refuse); an 8-bit output may also be
+# given as plain bytes
+_SEQ_TYPES = {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16, TYPE_E4M3: torch.float8_e4m3fn}
+_IDS = torch.int32, torch.int64
 
 
-def _of(name, code, *args):
-    """The addresses of (x, name)s, which as floating-point tensors have to be of the
-    type `code`; addresses and other memory are taken as they are."""
-    want = _SEQ_DTYPES[code] if 0 <= code < 3 else None  # an unknown code is the library's to refuse
-    out = []
-    for x, arg in args:
-        if isinstance(x, torch.Tensor) and want is not None and x.dtype is not want and x.dtype.is_floating_point:
-            raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {x.dtype}, described as {want}")
-        out.append(_addr(x))
+def _places(name, *args):
+    """The addresses of (x, arg, type)s.  Tensors have to be on the current device and of their type
+    if they are floating-point, integers of theirs side by side if that is an integer one; addresses
+    and other memory are taken as they are."""
+    out, here = [], None
+    for x, arg, want in args:
+        if not isinstance(x, torch.Tensor):
+            out.append(_addr(x))
+            continue
+        t = x.dtype
+        if want in _IDS and not (t is want and x.is_contiguous()):
+            raise CkptError(E_INVALID, f"{name}({arg}): {t} of strides {x.stride()}, not contiguous {want}")
+        if t is not want and t.is_floating_point and want is not None:
+            raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {t}, described as {want}")
+        if x.get_device() != here:
+            here = torch.cuda.current_device() if x.is_cuda else None
+            if x.get_device() != here:
+                raise CkptError(E_INVALID, f"{name}({arg}): a tensor on {x.device}, not on the current device")
+        out.append(x.data_ptr())
     return out
-
-
-def _ints(name, bits, *args):
-    """The addresses of (x, name)s, which as tensors have to be integers of `bits` bits side by side."""
-    want = torch.int64 if bits == 64 else torch.int32
-    for x, arg in args:
-        if isinstance(x, torch.Tensor) and (x.dtype is not want or not x.is_contiguous()):
-            raise CkptError(E_INVALID, f"{name}({arg}): {x.dtype} of strides {x.stride()}, not contiguous {want}")
-    return [_addr(x) for x, _ in args]
 
 
 def rms_desc(rows, c, xtype=TYPE_BF16, htype=None, ytype=None, gtype=None, dtype=None, qgroup=0, ldx=0, ldh=0, ldy=0,
@@ -882,17 +885,17 @@ def rms_desc(rows, c, xtype=TYPE_BF16, htype=None, ytype=None, gtype=None, dtype
 
 
 def op_rms_forward(desc: RmsDesc, x, w, y, st, res=None, h=None, ys=None, stream=None):
-    n = "op_rms_forward"
-    (px,), (pr, ph), (py,) = (_of(n, desc.xtype, (x, "x")), _of(n, desc.htype, (res, "res"), (h, "h")),
-                              _of(n, desc.ytype, (y, "y")))
-    pw, ps, pq = _of(n, TYPE_F32, (w, "w"), (st, "st"), (ys, "ys"))
+    ht = _SEQ_TYPES.get(desc.htype)
+    px, pr, pw, ph, py, pq, ps = _places(
+        "op_rms_forward", (x, "x", _SEQ_TYPES.get(desc.xtype)), (res, "res", ht), (w, "w", _F32), (h, "h", ht),
+        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _F32), (st, "st", _F32))
     _check(_lib.op_rms_forward(desc, px, pr, pw, ph, py, pq, ps, _s(stream)))
 
 
 def op_rms_apply(desc: RmsDesc, h, st, w, y, ys=None, stream=None):
-    n = "op_rms_apply"
-    (ph,), (py,) = _of(n, desc.htype, (h, "h")), _of(n, desc.ytype, (y, "y"))
-    pw, ps, pq = _of(n, TYPE_F32, (w, "w"), (st, "st"), (ys, "ys"))
+    ph, ps, pw, py, pq = _places(
+        "op_rms_apply", (h, "h", _SEQ_TYPES.get(desc.htype)), (st, "st", _F32), (w, "w", _F32),
+        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _F32))
     _check(_lib.op_rms_apply(desc, ph, ps, pw, py, pq, _s(stream)))
 
 
@@ -903,12 +906,11 @@ def op_rms_workspace_bytes(desc: RmsDesc) -> int:
 
 
 def op_rms_backward(desc: RmsDesc, g, h, st, w, d, dw, workspace, workspace_bytes, gh=None, stream=None):
-    n = "op_rms_backward"
-    (pg,), (ph,), (pe, pd) = (_of(n, desc.gtype, (g, "g")), _of(n, desc.htype, (h, "h")),
-                              _of(n, desc.dtype, (gh, "gh"), (d, "d")))
-    ps, pw, pdw = _of(n, TYPE_F32, (st, "st"), (w, "w"), (dw, "dw"))
-    _check(_lib.op_rms_backward(desc, pg, pe, ph, ps, pw, pd, pdw, _addr(workspace), _nbytes(workspace_bytes),
-                                _s(stream)))
+    dt = _SEQ_TYPES.get(desc.dtype)
+    pg, pe, ph, ps, pw, pd, pdw, ws = _places(
+        "op_rms_backward", (g, "g", _SEQ_TYPES.get(desc.gtype)), (gh, "gh", dt), (h, "h", _SEQ_TYPES.get(desc.htype)),
+        (st, "st", _F32), (w, "w", _F32), (d, "d", dt), (dw, "dw", _F32), (workspace, "workspace", None))
+    _check(_lib.op_rms_backward(desc, pg, pe, ph, ps, pw, pd, pdw, ws, _nbytes(workspace_bytes), _s(stream)))
 
 
 def embed_desc(tokens, vocab, c, wtype=TYPE_BF16, ytype=None, gtype=None, dtype=TYPE_F32, scale=1.0, ids64=False,
@@ -924,9 +926,8 @@ def embed_desc(tokens, vocab, c, wtype=TYPE_BF16, ytype=None, gtype=None, dtype=
 
 
 def op_embed_forward(desc: EmbedDesc, ids, w, y, stream=None):
-    n = "op_embed_forward"
-    (pi,), (pw,), (py,) = (_ints(n, 64 if desc.ids64 else 32, (ids, "ids")), _of(n, desc.wtype, (w, "w")),
-                           _of(n, desc.ytype, (y, "y")))
+    pi, pw, py = _places("op_embed_forward", (ids, "ids", _IDS[desc.ids64 != 0]), (w, "w", _SEQ_TYPES.get(desc.wtype)),
+                         (y, "y", _SEQ_TYPES.get(desc.ytype)))
     _check(_lib.op_embed_forward(desc, pi, pw, py, _s(stream)))
 
 
@@ -937,10 +938,10 @@ def op_embed_workspace_bytes(desc: EmbedDesc) -> int:
 
 
 def op_embed_backward(desc: EmbedDesc, ids, g, dw, workspace, workspace_bytes, stream=None):
-    n = "op_embed_backward"
-    (pi,), (pg,), (pd,) = (_ints(n, 64 if desc.ids64 else 32, (ids, "ids")), _of(n, desc.gtype, (g, "g")),
-                           _of(n, desc.dtype, (dw, "dw")))
-    _check(_lib.op_embed_backward(desc, pi, pg, pd, _addr(workspace), _nbytes(workspace_bytes), _s(stream)))
+    pi, pg, pd, ws = _places("op_embed_backward", (ids, "ids", _IDS[desc.ids64 != 0]),
+                             (g, "g", _SEQ_TYPES.get(desc.gtype)), (dw, "dw", _SEQ_TYPES.get(desc.dtype)),
+                             (workspace, "workspace", None))
+    _check(_lib.op_embed_backward(desc, pi, pg, pd, ws, _nbytes(workspace_bytes), _s(stream)))
 
 
 def attn_desc(tq, tk, seqs, heads, kv_heads, dim, causal=True, scale=0.0, ldq=0, hsq=0, ldk=0, hsk=0, ldv=0, hsv=0,
@@ -958,18 +959,19 @@ def op_attn_workspace_bytes(desc: AttnDesc, backward: bool) -> int:
 
 
 def op_attn_forward(desc: AttnDesc, q, k, v, qoff, koff, o, lse, workspace=None, workspace_bytes=0, stream=None):
-    n = "op_attn_forward"
-    pq, pk, pv, po = _of(n, TYPE_BF16, (q, "q"), (k, "k"), (v, "v"), (o, "o"))
-    (pl,), (pa, pb) = _of(n, TYPE_F32, (lse, "lse")), _ints(n, 32, (qoff, "qoff"), (koff, "koff"))
-    _check(_lib.op_attn_forward(desc, pq, pk, pv, pa, pb, po, pl, _addr(workspace), _nbytes(workspace_bytes),
-                                _s(stream)))
+    bf, i32 = torch.bfloat16, torch.int32
+    pq, pk, pv, pa, pb, po, pl, ws = _places(
+        "op_attn_forward", (q, "q", bf), (k, "k", bf), (v, "v", bf), (qoff, "qoff", i32), (koff, "koff", i32), (o, "o", bf),
+        (lse, "lse", _F32), (workspace, "workspace", None))
+    _check(_lib.op_attn_forward(desc, pq, pk, pv, pa, pb, po, pl, ws, _nbytes(workspace_bytes), _s(stream)))
 
 
 def op_attn_backward(desc: AttnDesc, g, q, k, v, o, lse, qoff, koff, dq, dk, dv, workspace, workspace_bytes,
                      stream=None):
-    n = "op_attn_backward"
-    pg, pq, pk, pv, po, pdq, pdk, pdv = _of(n, TYPE_BF16, (g, "g"), (q, "q"), (k, "k"), (v, "v"), (o, "o"), (dq, "dq"),
-                                            (dk, "dk"), (dv, "dv"))
-    (pl,), (pa, pb) = _of(n, TYPE_F32, (lse, "lse")), _ints(n, 32, (qoff, "qoff"), (koff, "koff"))
-    _check(_lib.op_attn_backward(desc, pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, _addr(workspace),
-                                 _nbytes(workspace_bytes), _s(stream)))
+    bf, i32 = torch.bfloat16, torch.int32
+    pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, ws = _places(
+        "op_attn_backward", (g, "g", bf), (q, "q", bf), (k, "k", bf), (v, "v", bf), (o, "o", bf), (lse, "lse", _F32),
+        (qoff, "qoff", i32), (koff, "koff", i32), (dq, "dq", bf), (dk, "dk", bf), (dv, "dv", bf),
+        (workspace, "workspace", None))
+    _check(_lib.op_attn_backward(desc, pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, ws, _nbytes(workspace_bytes),
+                                 _s(stream)))

@@ -220,6 +220,19 @@ def test_attention_arguments():
     refused(K.E_INVALID, K.attn_desc, 10, 12, 2, 4, 2, -(1 << 40))
 
 
+def test_tensors_of_another_device():
+    """Host memory would be a fault on the GPU."""
+    z = torch.zeros(16 * 16, dtype=torch.bfloat16)
+    f, i = torch.zeros(16), torch.zeros(16, dtype=torch.int32)
+    for bad in ((z, A, A, A), (A, f, A, A), (A, A, z, A), (A, A, A, f)):
+        refused(K.E_INVALID, K.op_rms_forward, K.rms_desc(4, 16), *bad)
+    for bad in ((i, A, A), (A, z, A), (A, A, z)):
+        refused(K.E_INVALID, K.op_embed_forward, K.embed_desc(5, 9, 16), *bad)
+    d = K.attn_desc(10, 12, 2, 4, 2, 16)
+    for bad in ((z, A, A, A, A, A, A), (A, A, A, i, A, A, A), (A, A, A, A, A, A, f), (A, A, A, A, A, A, A, z)):
+        refused(K.E_INVALID, K.op_attn_forward, d, *bad)
+
+
 def test_descriptors_match_the_header():
     """Sizes of the structures as the library's compiler lays them out: a field shifted by
     a missing one would be refused or read as another."""
