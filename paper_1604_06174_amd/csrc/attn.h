@@ -202,12 +202,14 @@ struct Places {
   int row;     // byte offset of chunk lane / 32 of row lane % 32; chunk 2 kk further on: ^ kk << 5
   int lo, hi;  // of the transposing reads of columns 0 .. 31; 32 b columns further on: ^ b << 6
 
-  __device__ __forceinline__ Places() {
+  __device__ __forceinline__ explicit Places(int columns = 0) {  // (a power of two, or 0) times 32 columns further on
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     row = r * D * 2 + ((swizzle<D>(r) ^ h) << 4);
     const int chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), r0 = 4 * h + ((lane >> 2) & 3), r1 = r0 + 8;
     lo = r0 * D * 2 + ((chunk ^ swizzle<D>(r0)) << 4) + (lane & 1) * 8;
     hi = r1 * D * 2 + ((chunk ^ swizzle<D>(r1)) << 4) + (lane & 1) * 8;
+    lo ^= columns << 6;
+    hi ^= columns << 6;
   }
   // A copy that the compiler takes for new values.  A tile's address in LDS is then an offset
   // within the reads; otherwise its sum with every place is formed before the loop, and
@@ -292,24 +294,24 @@ __device__ __forceinline__ void scrub(unsigned char *tile, int &special) {
 }
 
 // acc += (values of the 16 rows of the tile from `first` on, transposed) b
-template <int D>
-__device__ __forceinline__ void add_rows(f32x16 (&acc)[D / 32], const Places<D> &at, const unsigned char *tile,
-                                         int first, bf16x8 b) {
+template <int D, int N>
+__device__ __forceinline__ void add_rows(f32x16 (&acc)[N], const Places<D> &at, const unsigned char *tile, int first,
+                                         bf16x8 b) {
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t) acc[t] = mfma(at.columns(tile, first, t), b, acc[t]);
+  for (int t = 0; t < N; ++t) acc[t] = mfma(at.columns(tile, first, t), b, acc[t]);
 }
 
 // What scrub took out of rows row0 .. row1 - 1 of a matrix whose row r is at src + r ld; sees(r): does
 // the lane's row see it?  A probability times an infinity or a NaN is that
 // infinity or NaN (it is positive, however small); a score's gradient times one is a NaN, for
 // the score itself is then infinite or NaN (nan = true).
-template <int D, typename F>
-__device__ __forceinline__ void add_special(f32x16 (&acc)[D / 32], const __bf16 *src, int64_t ld, int dim, int row0,
-                                            int row1, bool nan, F &&sees) {
+template <int N, typename F>
+__device__ __forceinline__ void add_special(f32x16 (&acc)[N], const __bf16 *src, int64_t ld, int dim, int row0, int row1,
+                                            bool nan, F &&sees) {
   for (int r = row0; r < row1; ++r) {
     if (!sees(r)) continue;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int col = 32 * t + 8 * (i / 4) + 4 * ((threadIdx.x & 63) >> 5) + i % 4;

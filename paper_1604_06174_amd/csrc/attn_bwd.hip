@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs A, int tiles) {
     work(it, place ? kt1 : kt0, place ? vt1 : vt0, masked);
   });
   if (end > 0 && special)
-    add_special<D>(dq, kp, A.ldk, A.dim, full * BN, min(end * BN, sq.lk), true, [&](int j) { return j < lim; });
+    add_special(dq, kp, A.ldk, A.dim, full * BN, min(end * BN, sq.lk), true, [&](int j) { return j < lim; });
   if (valid) store_row(A.dq + (sq.q0 + token) * A.ldq + head * A.hsq, dq, A.scale, A.dim);
 }
 
@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {
       auto sees = [&](int r) { return r >= from; };
       // the tiles with tests: an odd one of the others, which comes just before them, is taken so too
       const int row0 = begin * BN, row1 = min(sq.lq, (seen + (h == heads - 1 && (whole & 1))) * BN);
-      add_special<D>(dv, A.g + sq.q0 * A.ldo + (head0 + h) * A.hso, A.ldo, A.dim, row0, row1, false, sees);
-      add_special<D>(dk, A.q + sq.q0 * A.ldq + (head0 + h) * A.hsq, A.ldq, A.dim, row0, row1, true, sees);
+      add_special(dv, A.g + sq.q0 * A.ldo + (head0 + h) * A.hso, A.ldo, A.dim, row0, row1, false, sees);
+      add_special(dk, A.q + sq.q0 * A.ldq + (head0 + h) * A.hsq, A.ldq, A.dim, row0, row1, true, sees);
     }
   if (!valid) return;
   if (A.parts > 1) {

@@ -121,12 +121,12 @@ __device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, i
   part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : factor / l);
 }
 
-// A wavefront's 32 rows as 32 keys after the other go by.
-template <int D>
+// A wavefront's 32 rows as 32 keys after the other go by; of o it forms 32 N columns.
+template <int D, int N>
 struct Rows {
-  static constexpr int T = D / 32, KK = D / 16;
+  static constexpr int KK = D / 16;
   bf16x8 q[KK];
-  f32x16 o[T];
+  f32x16 o[N];
   Sums z;
 
   __device__ __forceinline__ Rows(const AttnArgs &A, const __bf16 *query) : z(A.scale * LOG2E) {
@@ -153,7 +153,7 @@ struct Rows {
     if (z.rises(halves_max(top))) {
       const float f = z.move();
 #pragma unroll
-      for (int t = 0; t < T; ++t)
+      for (int t = 0; t < N; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= f;
     }
@@ -166,7 +166,7 @@ struct Rows {
     for (int c = 0; c < 2; ++c) {
       const bf16x8 p = operand(s[0], c);
       z.add_rounded(p);
-      add_rows<D>(o, at, vt, first + 16 * c, p);
+      add_rows(o, at, vt, first + 16 * c, p);
     }
   }
 };
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   int begin, end;
   b.share(A, (y.kend + BN - 1) / BN, begin, end);
 
-  Rows<D> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
+  Rows<D, D / 32> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
   const Places<D> places;
   const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
   const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
@@ -227,19 +227,19 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
                   r.template turn<MASKED>(places.here(), kt, vt, 0, y.lim - it * BN);
                 });
   if (begin < end && special)
-    add_special<D>(r.o, vp, A.ldv, A.dim, scrubbed * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
+    add_special(r.o, vp, A.ldv, A.dim, scrubbed * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
   const float factor = r.z.end();
   if (y.valid)
     finish(A, b.split, y.head, y.sq.q0 + y.token, r.z.base, r.z.l, factor, true,
            [&](auto *row, float scale) { store_row(row, r.o, scale, A.dim); });
 }
 
-// Four wavefronts with the same 32 rows: each takes a quarter of tiles of 128 keys, and their sums are
-// joined at the end.  Bound by HBM, with about 7 us of a workgroup's own at its start and end (16 single
-// tokens, 32/8 heads of 128, up to 8192 keys: 75 us, 4.0 TB/s; all of 4096 keys 5.0 TB/s).
+// Four wavefronts with the same 32 rows and tiles of 64 keys: two take 32 of the keys each, and half of o's
+// columns (forming the same scores twice, which costs a call that HBM bounds nothing), and the sums over the keys
+// are joined at the end.
 template <int D>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
-  constexpr int BM = 32, BN = 128, T = D / 32;
+  constexpr int BM = 32, BN = 64, T = D / 32, N = T / 2;
   __shared__ __align__(16) unsigned char kt0[BN * D * 2], kt1[BN * D * 2], vt0[BN * D * 2], vt1[BN * D * 2];
   __shared__ int special;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -250,48 +250,46 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   int begin, end;
   b.share(A, (y.kend + BN - 1) / BN, begin, end);
 
-  Rows<D> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
-  const Places<D> places;
+  const int part = wave & 1, columns = (wave >> 1) * N;  // its keys of a tile and its columns / 32
+  Rows<D, N> r(A, A.q + (y.sq.q0 + y.token) * A.ldq + y.head * A.hsq);
+  const Places<D> places(columns);
   const __bf16 *const vp = A.v + y.sq.k0 * A.ldv + b.kvh * A.hsv;
   const Loader<D, BN, 256> kload(A.k + y.sq.k0 * A.ldk + b.kvh * A.hsk, A.ldk, A.dim), vload(vp, A.ldv, A.dim);
   const int scrubbed =
       each_tile(kload, vload, begin, end, y.lim_lo, lk, kt0, kt1, vt0, vt1, special,
                 [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
-                  r.template turn<decltype(masked)::value>(places.here(), kt, vt, wave * 32, y.lim - it * BN - wave * 32);
+                  r.template turn<decltype(masked)::value>(places.here(), kt, vt, part * 32, y.lim - it * BN - part * 32);
                 });
   if (begin < end && special)
     for (int it = scrubbed; it < end; ++it)
-      add_special<D>(r.o, vp, A.ldv, A.dim, it * BN + wave * 32, min(it * BN + wave * 32 + 32, lk), false,
-                     [&](int j) { return j < y.lim; });
+      add_special(r.o, vp + 32 * columns, A.ldv, A.dim - 32 * columns, it * BN + part * 32,
+                  min(it * BN + part * 32 + 32, lk), false, [&](int j) { return j < y.lim; });
 
-  // The wavefronts' sums by their largest base: o (fp32, four values of a lane a place) goes through
-  // two of the tiles, and each wavefront adds up, and stores, 32 columns.
-  __shared__ float bases[4][32], ls[4][32], factors[4][32];
+  // The sums by their larger base: o (fp32, four values of a lane a place) goes through two of the tiles,
+  // and each wavefront adds up, and stores, 32 columns.
+  __shared__ float bases[2][32], ls[2][32], factors[2][32];
   tile_barrier();
-  auto place = [&](int w, int t, int c) {
-    return reinterpret_cast<float4 *>(w < 2 ? kt0 : vt0) + (((w & 1) * T + t) * 4 + c) * 64 + lane;
-  };
+  auto place = [&](int w, int t, int c) { return reinterpret_cast<float4 *>(w ? vt0 : kt0) + (t * 4 + c) * 64 + lane; };
 #pragma unroll
-  for (int t = 0; t < T; ++t)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      *place(wave, t, c) = make_float4(r.o[t][4 * c], r.o[t][4 * c + 1], r.o[t][4 * c + 2], r.o[t][4 * c + 3]);
+      *place(part, columns + t, c) = make_float4(r.o[t][4 * c], r.o[t][4 * c + 1], r.o[t][4 * c + 2], r.o[t][4 * c + 3]);
   const float factor = r.z.end();
-  if (lane < 32) {
-    bases[wave][lane] = r.z.base;
-    ls[wave][lane] = r.z.l;
-    factors[wave][lane] = factor;
+  if (columns == 0 && lane < 32) {
+    bases[part][lane] = r.z.base;
+    ls[part][lane] = r.z.l;
+    factors[part][lane] = factor;
   }
   __syncthreads();
   if (wave >= T) return;
-  float base = bases[0][lane & 31], sum = 0.f;
-#pragma unroll
-  for (int w = 1; w < 4; ++w) base = fmaxf(base, bases[w][lane & 31]);
+  const float base = fmaxf(bases[0][lane & 31], bases[1][lane & 31]);
+  float sum = 0.f;
   f32x16 out;
 #pragma unroll
   for (int i = 0; i < 16; ++i) out[i] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < 2; ++w) {
     // a wavefront without keys has a factor of 0 and nothing but zeros
     const float f = exp2_fast(bases[w][lane & 31] - (base == -INFINITY ? 0.f : base));
     const float fo = f * factors[w][lane & 31];
