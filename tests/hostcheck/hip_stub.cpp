@@ -9,8 +9,8 @@
 // scratch); the bf16 GEMM's argument block is checked over the whole extent
 // each operand spans for the launch's shape, leading dimensions, operand forms,
 // gathers, epilogue and split count, and so are a group norm's tensors and the
-// records its launches leave.  Grid and block sizes are checked against the device
-// limits.  Errors are counted and the first few printed.
+// records its launches leave, and the token models' operators' tensors and workspaces.  Grid and
+// block sizes are checked against the device limits.  Errors are counted and the first few printed.
 #include <cxxabi.h>
 #include <hip/hip_runtime.h>
 
@@ -28,6 +28,7 @@
 #include "../../paper_1604_06174_amd/csrc/gemm_bf16_kernel.h"
 #include "../../paper_1604_06174_amd/csrc/gn.h"
 #include "../../paper_1604_06174_amd/csrc/kernel_args.h"
+#include "../../paper_1604_06174_amd/csrc/seq.h"
 
 namespace {
 
@@ -40,7 +41,7 @@ struct Region {
 };
 
 struct Param {
-  enum Kind { PTR, SCALAR, GEMM_BF16, CONV, WGRAD, GEMM_F32, GN, DROPOUT } kind;
+  enum Kind { PTR, SCALAR, GEMM_BF16, CONV, WGRAD, GEMM_F32, GN, DROPOUT, RMS, RMS_BWD, EMBED, ATTN } kind;
 };
 
 struct KernelInfo {
@@ -193,6 +194,10 @@ void parse(KernelInfo &k) {
     else if (t == "ckpt::WgArgs") q.kind = Param::WGRAD;
     else if (t == "ckpt::GemmArgs") q.kind = Param::GEMM_F32;
     else if (t == "ckpt::GnArgs") q.kind = Param::GN;
+    else if (t == "ckpt::RmsArgs") q.kind = Param::RMS;
+    else if (t == "ckpt::RmsBwdArgs") q.kind = Param::RMS_BWD;
+    else if (t == "ckpt::EmbedArgs") q.kind = Param::EMBED;
+    else if (t == "ckpt::AttnArgs") q.kind = Param::ATTN;
     else if (t == "ckpt::(anonymous namespace)::Args" && p.find("k_dropout<") != std::string::npos)
       q.kind = Param::DROPOUT;
     else if (t == "int" || t == "long" || t == "unsigned int" || t == "unsigned long" || t == "float" ||
@@ -354,6 +359,99 @@ void check_gn(const KernelInfo &k, const ckpt::GnArgs &a) {
   if (a.drop.rng) check_extent(k, "seed and step", a.drop.rng, 16);
 }
 
+// bytes of the i-th template argument
+uint64_t targ_size(const KernelInfo &k, size_t i) {
+  const std::string t = i < k.targs.size() ? k.targs[i] : "";
+  return t == "float" ? 4 : t.find("E4m3") != std::string::npos ? 1 : 2;
+}
+
+void check_rms(const KernelInfo &k, const ckpt::RmsArgs &a) {
+  const uint64_t rows = a.rows, c = a.c;
+  const bool res = k.targs[3] == "true", apply = k.targs[4] == "true";
+  check_extent(k, "x", a.x, rows_span(rows, apply ? a.ldh : a.ldx, c) * targ_size(k, 0));
+  if (res) {
+    check_extent(k, "res", a.res, rows_span(rows, a.ldh, c) * targ_size(k, 1));
+    check_extent(k, "h", a.h, rows_span(rows, a.ldh, c) * targ_size(k, 1));
+  }
+  check_extent(k, "y", a.y, rows_span(rows, a.ldy, c) * targ_size(k, 2));
+  if (targ_size(k, 2) == 1) check_extent(k, "ys", a.ys, rows * a.groups * 4);
+  check_extent(k, "st", a.st, rows * 4);
+  check_extent(k, "w", a.w, c * 4);
+}
+
+void check_rms_bwd(const KernelInfo &k, const ckpt::RmsBwdArgs &a, dim3 grid) {
+  const uint64_t rows = a.rows, c = a.c;
+  check_extent(k, "g", a.g, rows_span(rows, a.ldg, c) * targ_size(k, 0));
+  check_extent(k, "h", a.h, rows_span(rows, a.ldh, c) * targ_size(k, 1));
+  if (a.gh) check_extent(k, "gh", a.gh, rows_span(rows, a.ldd, c) * targ_size(k, 2));
+  check_extent(k, "d", a.d, rows_span(rows, a.ldd, c) * targ_size(k, 2));
+  check_extent(k, "st", a.st, rows * 4);
+  check_extent(k, "w", a.w, c * 4);
+  check_extent(k, "records", a.part, uint64_t(grid.x) * a.cpad * 4);
+}
+
+void check_embed(const KernelInfo &k, const ckpt::EmbedArgs &a) {
+  auto is = [&](const char *name) { return k.pretty.find(name) != std::string::npos; };
+  const uint64_t n = a.tokens, v = a.vocab, c = a.c;
+  if (is("k_embed_forward<")) {
+    check_extent(k, "table", a.src, rows_span(v, a.lds, c) * targ_size(k, 0));
+    check_extent(k, "rows", a.dst, rows_span(n, a.ldd, c) * targ_size(k, 1));
+  }
+  if (is("k_embed_forward<") || is("k_embed_sort<")) check_extent(k, "ids", a.ids, n * (a.ids64 ? 8 : 4));
+  if (is("k_embed_forward<")) return;
+  check_extent(k, "start", a.start, (v + 1) * 4);
+  if (!is("k_embed_join<")) {
+    check_extent(k, "perm", a.perm, n * 4);
+    check_extent(k, "key", a.key, n * 4);
+  }
+  if (is("k_embed_sort<")) return;
+  const size_t dt = is("k_embed_sum<") ? 1 : 0;
+  if (is("k_embed_sum<")) check_extent(k, "gradient", a.src, rows_span(n, a.lds, c) * targ_size(k, 0));
+  check_extent(k, "table's gradient", a.dst, rows_span(v, a.ldd, c) * targ_size(k, dt));
+  check_extent(k, "tail", a.tail, uint64_t(a.chunks) * 4);
+  check_extent(k, "pieces", a.part, uint64_t(a.chunks) * 2 * a.cpad * 4);
+}
+
+void check_attn(const KernelInfo &k, const ckpt::AttnArgs &a) {
+  auto is = [&](const char *name) { return k.pretty.find(name) != std::string::npos; };
+  auto heads = [&](const char *what, const void *p, uint64_t rows, int64_t ld, int64_t n, int64_t hs) {
+    if (rows) check_extent(k, what, p, ((rows - 1) * ld + (n - 1) * hs + a.dim) * 2);
+  };
+  const bool fwd = is("k_attn_many<") || is("k_attn_few<"), dq = is("k_attn_dq<"), dkv = is("k_attn_dkv<"),
+             join = is("k_attn_join("), sum = is("k_attn_heads(");
+  const uint64_t rows = uint64_t(a.heads) * a.tq, split = uint64_t(a.splits) * rows;
+  if (fwd || dq || dkv) {
+    heads("q", a.q, a.tq, a.ldq, a.heads, a.hsq);
+    heads("k", a.k, a.tk, a.ldk, a.kv_heads, a.hsk);
+    heads("v", a.v, a.tk, a.ldv, a.kv_heads, a.hsv);
+  }
+  if (!sum) check_extent(k, "qoff", a.qoff, 4 * (uint64_t(a.seqs) + 1));
+  if (!join) check_extent(k, "koff", a.koff, 4 * (uint64_t(a.seqs) + 1));
+  if (fwd || join) {
+    if (a.splits > 1) {
+      check_extent(k, "splits' sums", a.pml, split * 8);
+      check_extent(k, "splits' outputs", a.po, split * a.dim * 4);
+    }
+    heads("o", a.o, a.tq, a.ldo, a.heads, a.hso);
+    check_extent(k, "lse", a.lse, rows * 4);
+  }
+  if (dq || dkv) {
+    heads("g", a.g, a.tq, a.ldo, a.heads, a.hso);
+    check_extent(k, "delta", a.delta, rows * 4);
+    check_extent(k, "lse in base 2", a.lse2, rows * 4);
+  }
+  if (dq) {
+    heads("o", a.out, a.tq, a.ldo, a.heads, a.hso);
+    heads("dq", a.dq, a.tq, a.ldq, a.heads, a.hsq);
+    check_extent(k, "lse", a.lse, rows * 4);
+  }
+  if (dkv || sum) {
+    heads("dk", a.dk, a.tk, a.ldk, a.kv_heads, a.hsk);
+    heads("dv", a.dv, a.tk, a.ldv, a.kv_heads, a.hsv);
+    if (a.parts > 1) check_extent(k, "parts", a.pkv, 2 * uint64_t(a.parts) * a.tk * a.kv_heads * a.dim * 4);
+  }
+}
+
 void check_launch(const void *f, dim3 grid, dim3 block, void **args, size_t shm) {
   std::lock_guard<std::mutex> lock(S().mu);
   ++S().launches;
@@ -371,6 +469,7 @@ void check_launch(const void *f, dim3 grid, dim3 block, void **args, size_t shm)
     error(k.pretty + ": grid " + std::to_string(grid.x) + "x" + std::to_string(grid.y) + "x" +
           std::to_string(grid.z) + " outside the device limits");
   const uint64_t threads = uint64_t(block.x) * block.y * block.z;
+  if (uint64_t(grid.x) * block.x >> 32) error(k.pretty + ": a launch of 2^32 threads or more along x");
   if (threads == 0 || threads > 1024) error(k.pretty + ": block of " + std::to_string(threads) + " threads");
   if (shm > 160 * 1024) error(k.pretty + ": " + std::to_string(shm) + " bytes of dynamic LDS");
   for (size_t i = 0; i < k.params.size(); ++i) {
@@ -396,6 +495,10 @@ void check_launch(const void *f, dim3 grid, dim3 block, void **args, size_t shm)
         break;
       }
       case Param::GN: check_gn(k, *static_cast<const ckpt::GnArgs *>(args[i])); break;
+      case Param::RMS: check_rms(k, *static_cast<const ckpt::RmsArgs *>(args[i])); break;
+      case Param::RMS_BWD: check_rms_bwd(k, *static_cast<const ckpt::RmsBwdArgs *>(args[i]), grid); break;
+      case Param::EMBED: check_embed(k, *static_cast<const ckpt::EmbedArgs *>(args[i])); break;
+      case Param::ATTN: check_attn(k, *static_cast<const ckpt::AttnArgs *>(args[i])); break;
       case Param::DROPOUT: {  // three tensors first
         for (int q = 0; q < 3; ++q) check_ptr(k, "a dropout tensor", static_cast<void *const *>(args[i])[q]);
         break;
