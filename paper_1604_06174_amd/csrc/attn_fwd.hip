@@ -199,7 +199,7 @@ __device__ __forceinline__ int each_tile(const Loader<D, BN, 256> &kload, const 
 
 // Four wavefronts of 32 rows share tiles of 32 keys, which leaves room for three of them on each SIMD.
 // Bound by the vector and matrix units together, and by power (16384 tokens, 16/4 heads of 128 in seven
-// sequences: 226 us, 894 TFLOP/s of the visible products, at 2.0 GHz; the library's largest bf16 products
+// sequences: 230 us, 880 TFLOP/s of the visible products, at 2.0 GHz; the library's largest bf16 products
 // reach 1300).  Tiles of 64 keys with two wavefronts took 4% longer, and so did the scores, exponentials
 // and values of three turns side by side; 64 rows a wavefront, one a SIMD, 25%.
 template <int D>
@@ -212,6 +212,7 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
   Query<BM> y;
   if (!y.find(A, tiles, b.tile, b.kvh, wave * 32 + (lane & 31))) return;
   const int lk = y.sq.lk, lim_hi = __builtin_amdgcn_readlane(y.lim, 31);  // the wavefront's most
+  const bool idle = y.sq.first + wave * 32 >= y.rows;
   int begin, end;
   b.share(A, (y.kend + BN - 1) / BN, begin, end);
 
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
       each_tile(kload, vload, begin, end, y.lim_lo, lk, kt0, kt1, vt0, vt1, special,
                 [&](int it, const unsigned char *kt, const unsigned char *vt, auto masked) __attribute__((always_inline)) {
                   constexpr bool MASKED = decltype(masked)::value;
-                  if (MASKED && it * BN >= lim_hi) return;  // nothing for the wavefront's rows
+                  if (idle || (MASKED && it * BN >= lim_hi)) return;  // nothing for the wavefront's rows
                   r.template turn<MASKED>(places.here(), kt, vt, 0, y.lim - it * BN);
                 });
   if (begin < end && special)
@@ -236,7 +237,9 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
 
 // Four wavefronts with the same 32 rows and tiles of 64 keys: two take 32 of the keys each, and half of o's
 // columns (forming the same scores twice, which costs a call that HBM bounds nothing), and the sums over the keys
-// are joined at the end.
+// are joined at the end.  Bound by HBM: 16 single tokens, 32/8 heads of 128, up to 8192 keys, 68 us and 5 for
+// k_attn_join, 4.4 TB/s.  Tiles of 128 keys, a quarter of them a wavefront's, leave room for one workgroup on
+// a compute unit, and its start and end (7 us) are not covered: 71.
 template <int D>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   constexpr int BM = 32, BN = 64, T = D / 32, N = T / 2;
@@ -308,37 +311,48 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
            [&](auto *row, float scale) { store_tile(row, out, wave, scale, A.dim); });
 }
 
-// a row's splits joined: sixteen lanes a row, eight columns each
+// A row's splits joined: a wavefront a row, lane z with the sums of split z (there are at most 64), then
+// sixteen lanes with eight columns each for every fourth split.
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
-  const int64_t at = blockIdx.x * int64_t(16) + threadIdx.x / 16, n = A.heads * A.tq;
+  const int64_t at = blockIdx.x * int64_t(4) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = A.heads * A.tq;
   if (at >= n) return;
   const int64_t token = at % A.tq;
-  const int head = int(at / A.tq), col = (threadIdx.x & 15) * 8;
+  const int lane = threadIdx.x & 63, head = int(at / A.tq), col = (lane & 15) * 8, quarter = lane >> 4;
   // rows of no sequence have no splits either
   if (token < A.qoff[0] || token >= A.qoff[A.seqs]) return;
-  float top = -INFINITY;
-  for (int z = 0; z < A.splits; ++z) top = fmaxf(top, A.pml[2 * (z * n + at)]);
-  const float base = top == -INFINITY ? 0.f : top;
-  float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-  for (int z = 0; z < A.splits; ++z) {
-    const float lz = A.pml[2 * (z * n + at) + 1];
-    const float f = exp2_fast(A.pml[2 * (z * n + at)] - base);
-    if (lz == 0.f) continue;
-    l += lz * f;
-    if (col < A.dim) {
-      const float4 *const p = reinterpret_cast<const float4 *>(A.po + (z * n + at) * A.dim + col);
-      const float4 a = p[0], b = p[1];
-      o[0] += a.x * f, o[1] += a.y * f, o[2] += a.z * f, o[3] += a.w * f;
-      o[4] += b.x * f, o[5] += b.y * f, o[6] += b.z * f, o[7] += b.w * f;
-    }
+  float base = -INFINITY, l = 0.f;
+  if (lane < A.splits) {
+    base = A.pml[2 * (lane * n + at)];
+    l = A.pml[2 * (lane * n + at) + 1];
   }
-  if (col == 0) A.lse[at] = l == 0.f ? -INFINITY : fmaf(base, LN2, logf(l));
-  if (col < A.dim) {
+  float top = base;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if (top == -INFINITY) top = 0.f;
+  const float f = exp2_fast(base - top);  // 0 for a split without keys
+  l = f == 0.f ? 0.f : l * f;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const bool ok = col < A.dim;
+#pragma unroll 4
+  for (int z0 = 0; z0 < A.splits; z0 += 4) {
+    const int z = z0 + quarter;
+    const float fz = __shfl(f, z);
+    if (!ok || fz == 0.f) continue;
+    const float4 *const p = reinterpret_cast<const float4 *>(A.po + (z * n + at) * A.dim + col);
+    const float4 a = p[0], b = p[1];
+    s[0] = fmaf(a.x, fz, s[0]), s[1] = fmaf(a.y, fz, s[1]), s[2] = fmaf(a.z, fz, s[2]), s[3] = fmaf(a.w, fz, s[3]);
+    s[4] = fmaf(b.x, fz, s[4]), s[5] = fmaf(b.y, fz, s[5]), s[6] = fmaf(b.z, fz, s[6]), s[7] = fmaf(b.w, fz, s[7]);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s[k] = xor_add<32>(xor_add<16>(s[k]));
+  if (lane == 0) A.lse[at] = l == 0.f ? -INFINITY : fmaf(top, LN2, logf(l));
+  if (ok && quarter == 0) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     bf16x8 r;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) r[k] = (__bf16)(o[k] * inv);
+    for (int k = 0; k < 8; ++k) r[k] = (__bf16)(s[k] * inv);
     *reinterpret_cast<bf16x8 *>(A.o + token * A.ldo + head * A.hso + col) = r;
   }
 }
@@ -355,7 +369,7 @@ void forward(hipStream_t s, const AttnArgs &a) {
   else
     hipLaunchKernelGGL(k_attn_many<D>, grid, dim3(256), 0, s, a, tiles);
   if (a.splits > 1)
-    hipLaunchKernelGGL(k_attn_join, dim3(uint32_t((a.heads * a.tq + 15) / 16)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_attn_join, dim3(uint32_t((a.heads * a.tq + 3) / 4)), dim3(256), 0, s, a);
 }
 
 }  // namespace
