@@ -237,9 +237,9 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
 
 // Four wavefronts with the same 32 rows and tiles of 64 keys: two take 32 of the keys each, and half of o's
 // columns (forming the same scores twice, which costs a call that HBM bounds nothing), and the sums over the keys
-// are joined at the end.  Bound by HBM: 16 single tokens, 32/8 heads of 128, up to 8192 keys, 68 us and 5 for
-// k_attn_join, 4.4 TB/s.  Tiles of 128 keys, a quarter of them a wavefront's, leave room for one workgroup on
-// a compute unit, and its start and end (7 us) are not covered: 71.
+// are joined at the end.  Bound by HBM: 16 single tokens, 32/8 heads of 128, up to 8192 keys, 66 us in
+// all, 4.6 TB/s.  With tiles of 128 keys, a quarter of them a wavefront's, one workgroup fits a compute unit,
+// and its start and end (7 us) are not covered: 3 us more.
 template <int D>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
   constexpr int BM = 32, BN = 64, T = D / 32, N = T / 2;
@@ -357,6 +357,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   }
 }
 
+// Up to 32 rows a sequence on the average go to k_attn_few.  64 sequences of 1024 keys, 16 heads of 64: 32
+// rows each 60 us (by k_attn_many 58), 64 each 103 (62); one token, 8 heads of 128 against 2048 keys 13 (16),
+// 16 tokens of 32/8 heads against up to 8192 73 (75 to 81).
 bool few_rows(const AttnArgs &a) { return a.tq * a.rep <= int64_t(32) * a.seqs; }
 
 template <int D>
@@ -374,13 +377,16 @@ void forward(hipStream_t s, const AttnArgs &a) {
 
 }  // namespace
 
-// Workgroups for one another's keys where the rows alone fill less than two for each compute
-// unit; a split is 256 keys at least of a sequence of the average length.
+// Workgroups for one another's keys where the rows alone make less than three for each compute
+// unit; a split is 256 keys at least of a sequence of the average length.  768: 16 single tokens,
+// 32/8 heads of 128, against up to 8192 keys 66 us, against 4096 each 64; 512: 73, for the longest sequences
+// end last, and 60; 1024: 72 and 60.  256 keys: one token of 8 heads against 2048 13 us, of 32/8 heads
+// against 16384 26; 512 keys: 17 and 23.
 int attn_splits(const AttnArgs &a) {
   const int bm = few_rows(a) ? 32 : 128;
   const int64_t work = (a.tq * a.rep / bm > a.seqs ? a.tq * a.rep / bm : a.seqs) * a.kv_heads;
   const int64_t keys = a.tk / a.seqs / 256;
-  int64_t n = 512 / (work > 0 ? work : 1);
+  int64_t n = 768 / (work > 0 ? work : 1);
   n = n < keys ? n : keys;
   return int(n < 1 ? 1 : n > 64 ? 64 : n);
 }
