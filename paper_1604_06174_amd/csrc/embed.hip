@@ -33,6 +33,8 @@ namespace {
 
 constexpr int SECTIONS = 16;    // wavefronts of a sorting workgroup
 constexpr int LIST = 512;       // tokens of a section that are kept from the first reading
+// ids that a wavefront writes zeros for (16384 tokens of 32000 ids, 2048 columns: 98 us, with 64 128)
+constexpr int ABSENT = 16;
 constexpr int MAX_RANGE = 1024; // ids of one: [SECTIONS][MAX_RANGE] counts take 64 KB of LDS
 
 template <typename T>
@@ -266,12 +268,15 @@ __device__ __forceinline__ void put_row(const EmbedArgs &A, int v, int col, int 
 template <typename GT, typename DT>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int zeros) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (int(blockIdx.x) < zeros) {  // 64 ids a wavefront
-    const int64_t v0 = (blockIdx.x * int64_t(4) + wave) * 64, v = v0 + lane;
+  if (int(blockIdx.x) < zeros) {
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (uint64_t absent = __ballot(v < A.vocab && A.start[v] == A.start[v + 1]); absent; absent &= absent - 1) {
-      DT *const row = static_cast<DT *>(A.dst) + (v0 + __ffsll((unsigned long long)absent) - 1) * A.ldd;
-      for (int col = lane * 8; col < A.c; col += 512) store8(row + col, min(8, A.c - col), zero);
+    for (int64_t v0 = (blockIdx.x * int64_t(4) + wave) * ABSENT; v0 < A.vocab; v0 += int64_t(zeros) * 4 * ABSENT) {
+      const int64_t v = v0 + lane;
+      for (uint64_t absent = __ballot(lane < ABSENT && v < A.vocab && A.start[v] == A.start[v + 1]); absent;
+           absent &= absent - 1) {
+        DT *const row = static_cast<DT *>(A.dst) + (v0 + __ffsll((unsigned long long)absent) - 1) * A.ldd;
+        for (int col = lane * 8; col < A.c; col += 512) store8(row + col, min(8, A.c - col), zero);
+      }
     }
     return;
   }
@@ -279,19 +284,20 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, int tiles, int z
   const int64_t chunk = unit / tiles;
   if (chunk >= A.chunks) return;
   const int col = int(unit - chunk * tiles) * 512 + lane * 8, cnt = min(8, A.c - col);
-  const int total = A.start[A.vocab], P = A.chunk, p0 = int(min(chunk * P, int64_t(total))), p1 = min(p0 + P, total);
+  // all positions that may have to be added up here (what lies past the last, `total`, is not looked at)
+  const int total = A.start[A.vocab], P = A.chunk;
+  int tok[2] = {0, 0}, key[2] = {0, 0};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (const int64_t at = chunk * P + u * 64 + lane; at < A.tokens) {
+      tok[u] = A.perm[at];
+      key[u] = A.key[at];
+    }
+  const int p0 = int(min(chunk * P, int64_t(total))), p1 = min(p0 + P, total);
   if (p0 == p1) {
     if (lane == 0) A.tail[chunk] = -1;
     return;
   }
-  // all positions that may have to be added up here, while the ids at the chunk's ends are looked up
-  int tok[2] = {0, 0}, key[2] = {-1, -1};
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-    if (p0 + u * 64 + lane < total) {
-      tok[u] = A.perm[p0 + u * 64 + lane];
-      key[u] = A.key[p0 + u * 64 + lane];
-    }
   auto token_at = [&](int q) { return q < 64 ? __builtin_amdgcn_readlane(tok[0], q) : __builtin_amdgcn_readlane(tok[1], q - 64); };
   auto key_at = [&](int q) { return q < 64 ? __builtin_amdgcn_readlane(key[0], q) : __builtin_amdgcn_readlane(key[1], q - 64); };
   const int k0 = key_at(0), k1 = key_at(p1 - p0 - 1);
@@ -435,7 +441,8 @@ void backward(hipStream_t s, const EmbedArgs &a) {
     hipLaunchKernelGGL(k_embed_sort<true>, ranges, dim3(64 * SECTIONS), 0, s, a, range);
   else
     hipLaunchKernelGGL(k_embed_sort<false>, ranges, dim3(64 * SECTIONS), 0, s, a, range);
-  const int tiles = (a.c + 511) / 512, zeros = a.accumulate ? 0 : int((a.vocab + 255) / 256);
+  const int64_t need = (a.vocab + 4 * ABSENT - 1) / (4 * ABSENT);
+  const int tiles = (a.c + 511) / 512, zeros = a.accumulate ? 0 : int(need < 65536 ? need : 65536);
   hipLaunchKernelGGL((k_embed_sum<GT, DT>), dim3(uint32_t(zeros + (int64_t(a.chunks) * tiles + 3) / 4)), dim3(256), 0, s,
                      a, tiles, zeros);
   if (a.tokens > a.chunk)
@@ -456,7 +463,9 @@ void embed_forward(hipStream_t s, const EmbedArgs &a, int wtype, int ytype) {
 }
 
 uint64_t embed_plan(EmbedArgs &a, char *ws) {
-  // positions a wavefront begins with: 16 wavefronts for each compute unit, if there are as many
+  // positions a wavefront begins with: 16 wavefronts for each compute unit, if there are as many (65536 tokens,
+  // 1024 columns: 32 positions 117 us, 16 119, 64 120), but 16 at least, so that up to 16 tokens of an id are
+  // one running sum (4099 tokens of 97 ids, 333 columns: 27 us, with 8 positions 23)
   const int64_t tiles = (a.c + 511) / 512;
   a.chunk = 64;
   while (a.chunk > 16 && (a.tokens + a.chunk - 1) / a.chunk * tiles < 4096) a.chunk /= 2;
