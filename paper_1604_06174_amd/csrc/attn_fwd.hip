@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if (top == -INFINITY) top = 0.f;
   const float f = exp2_fast(base - top);  // 0 for a split without keys
-  l = f == 0.f ? 0.f : l * f;
+  l *= f;                                 // a NaN of a split stays one
 #pragma unroll
   for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};

@@ -330,6 +330,27 @@ def test_a_row_that_sees_one_key_gets_its_value(lens, heads, kv, dim):
     assert n >= 2
 
 
+@pytest.mark.parametrize("keys", [300, 1025, 3400, 15873, 16400])
+def test_numbers_of_splits(keys):
+    """1, 4, 13, 62 and 64 of them for one head."""
+    t = Case([(1, keys)], 1, 1, 64, seed=keys)
+    t.forward()
+    t.check_forward()
+
+
+@pytest.mark.parametrize("at,score", [(0, 0.0), (2000, 0.0), (4095, 0.0), (2000, 400.0)])
+def test_a_seen_nan_in_one_split(at, score):
+    """The only finite score of a split or not, and however far below another split's it is."""
+    t = Case([(1, 4096)], 2, 1, 64, seed=5)
+    t.d["q"].fill_(1.0)
+    t.d["k"].fill_(0.0)
+    t.d["k"][1000, 0] = score / 8
+    t.d["k"][at, 0, 3] = float("nan")
+    t.forward()
+    torch.cuda.synchronize()
+    assert bool(t.d["o"].isnan().all()) and bool(t.lse.isnan().all())
+
+
 def test_a_past_of_more_tiles_than_32_bits_hold():
     """Four single tokens of 128 heads on one key head, one of them behind 2^29 keys: one key has a
     score of 40 and the others of 0, so the answer is its value (they add 2^29 exp(-40) < 2^-28 of it)."""
