@@ -58,14 +58,18 @@ def visible(lq, lk, causal):
     return np.tril(seen, lk - lq) if causal else seen
 
 
-def _clean(seen, *mats):
-    """Hidden rows of a matrix play no part whatever they hold: with each row i of `seen`,
-    the matrix's rows that it does not see as zeros.  (Only for matrices that hold such.)"""
+def _finite(*mats):
     return [np.where(np.isfinite(m), m, 0.0) for m in mats]
 
 
+def _odd(m):
+    """Rows that hold an infinity or a NaN."""
+    return ~np.isfinite(m).all(1)
+
+
 def attention(q, k, v, qoff, koff, causal, scale):
-    """o [tq, heads, dim], lse [heads, tq] and their error bounds.  Rows of no sequence are NaN."""
+    """o [tq, heads, dim], lse [heads, tq] and their error bounds.  Rows of no sequence are NaN.
+    What a query does not see plays no part, whatever it holds; infinities and NaNs that it sees do."""
     tq, heads, dim = q.shape
     rep = heads // k.shape[1]
     o, eo = np.full((tq, heads, dim), np.nan), np.full((tq, heads, dim), np.nan)
@@ -75,10 +79,10 @@ def attention(q, k, v, qoff, koff, causal, scale):
         seen = visible(lq, lk, causal)
         for h in range(heads):
             Q, K, V = q[a:b, h], k[c:d, h // rep], v[c:d, h // rep]
-            Kf, Vf = _clean(seen, K, V)  # non-finite rows are hidden ones in the tests
-            e = np.where(seen, Q @ Kf.T * scale, -np.inf)
-            mag = np.where(seen, np.abs(Q) @ np.abs(Kf).T * scale, 0.0)
-            if lk == 0:
+            Qf, Kf, Vf = _finite(Q, K, V)
+            e = np.where(seen, Qf @ Kf.T * scale, -np.inf)
+            mag = np.where(seen, np.abs(Qf) @ np.abs(Kf).T * scale, 0.0)
+            if lk == 0 or lq == 0:
                 o[a:b, h], eo[a:b, h], lse[h, a:b], el[h, a:b] = 0, 1e-30, -np.inf, 0
                 continue
             top = e.max(1)
@@ -97,6 +101,13 @@ def attention(q, k, v, qoff, koff, causal, scale):
             # sum u p |v - o| <= u (sum p |v| + |o|), and rounded itself
             eo[a:b, h] = (U16 + 2 * rel)[:, None] * (p @ np.abs(Vf)) + 2 * U16 * np.abs(o[a:b, h]) + 1e-30
             el[h, a:b] = np.where(none, 0, rel + 4 * U24 * np.abs(np.where(none, 0, lse[h, a:b])))
+            # rows with infinities and NaNs, of the keys that they see alone
+            for i in np.flatnonzero((seen & (_odd(K) | _odd(V))).any(1) | (_odd(Q) & seen.any(1))):
+                with np.errstate(invalid="ignore", divide="ignore"):
+                    e = (Q[i] * K[seen[i]]).sum(1) * scale
+                    p = np.exp(e - e.max())
+                    o[a + i, h] = (p[:, None] * V[seen[i]]).sum(0) / p.sum()
+                    lse[h, a + i] = e.max() + np.log(p.sum())
     return o, lse, eo, el
 
 
@@ -116,11 +127,15 @@ def attention_backward(g, q, k, v, o, lse, qoff, koff, causal, scale):
             continue
         for h in range(heads):
             kh = h // rep
-            Q, K, V, G, O = _clean(seen, q[a:b, h], k[c:d, kh], v[c:d, kh], g[a:b, h], o[a:b, h])
+            raw = q[a:b, h], k[c:d, kh], v[c:d, kh], g[a:b, h], o[a:b, h]
+            Q, K, V, G, O = _finite(*raw)
             L = lse[h, a:b]
             fin = np.isfinite(L)
             Lf = np.where(fin, L, 0.0)
-            s = seen & fin[:, None]
+            # rows with infinities and NaNs are added below, of the keys that they see alone
+            s = seen & ~np.isneginf(L)[:, None]
+            odd = (s & (_odd(raw[1]) | _odd(raw[2]))).any(1) | _odd(raw[0]) | _odd(raw[3]) | _odd(raw[4]) | np.isnan(L)
+            rest, s = s & odd[:, None], s & fin[:, None] & ~odd[:, None]
             e = Q @ K.T * scale
             mag = np.abs(Q) @ np.abs(K).T * scale
             p = np.where(s, np.exp(np.where(s, e - Lf[:, None], 0.0)), 0.0)
@@ -137,6 +152,15 @@ def attention_backward(g, q, k, v, o, lse, qoff, koff, causal, scale):
             err[1][c:d, kh] += (eds + chain * np.abs(ds)).T @ np.abs(Q) * scale
             out[2][c:d, kh] += p.T @ G
             err[2][c:d, kh] += (ep + chain * p).T @ np.abs(G)
+            for i in np.flatnonzero(rest.any(1)):
+                n = rest[i]
+                Qi, Gi, Oi, Kn, Vn = raw[0][i], raw[3][i], raw[4][i], raw[1][n], raw[2][n]
+                with np.errstate(invalid="ignore", over="ignore"):
+                    p = np.exp((Qi * Kn).sum(1) * scale - L[i])[:, None]
+                    ds = p * ((Gi * Vn).sum(1) - (Gi * Oi).sum())[:, None] * scale
+                    out[0][a + i, h] += (ds * Kn).sum(0)
+                    out[1][c:d, kh][n] += ds * Qi
+                    out[2][c:d, kh][n] += p * Gi
     for t, e in zip(out, err):
         e += U16 * np.abs(t) + 1e-30
     return out, err

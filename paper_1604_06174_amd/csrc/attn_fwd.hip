@@ -312,7 +312,8 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 }
 
 // A row's splits joined: a wavefront a row, lane z with the sums of split z (there are at most 64), then
-// sixteen lanes with eight columns each for every fourth split.
+// sixteen lanes with eight columns each for every fourth split.  Every split is added, however small
+// its factor: an infinity or a NaN that its keys' values left in its columns stands nowhere else.
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   const int64_t at = blockIdx.x * int64_t(4) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = A.heads * A.tq;
   if (at >= n) return;
@@ -329,17 +330,16 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if (top == -INFINITY) top = 0.f;
-  const float f = exp2_fast(base - top);  // 0 for a split without keys
+  const float f = exp2_fast(base - top);  // 0 for a split without keys, which left zeros
   l *= f;                                 // a NaN of a split stays one
 #pragma unroll
   for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const bool ok = col < A.dim;
-#pragma unroll 4
   for (int z0 = 0; z0 < A.splits; z0 += 4) {
     const int z = z0 + quarter;
     const float fz = __shfl(f, z);
-    if (!ok || fz == 0.f) continue;
+    if (!ok || z >= A.splits) continue;
     const float4 *const p = reinterpret_cast<const float4 *>(A.po + (z * n + at) * A.dim + col);
     const float4 a = p[0], b = p[1];
     s[0] = fmaf(a.x, fz, s[0]), s[1] = fmaf(a.y, fz, s[1]), s[2] = fmaf(a.z, fz, s[2]), s[3] = fmaf(a.w, fz, s[3]);

@@ -1,0 +1,78 @@
+"""Attention over packed sequences (op_attn_*) where values go to their limits: special values, in split
+keys too.  Against the float64 oracle (oracle.seq)."""
+import numpy as np
+import pytest
+
+from oracle import seq as S
+from seq_cases import host, rounded
+from test_gpu_attn import SAME, Case
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+# rows for each of the forward's forms: tiles of 128, of 32, and keys split over workgroups
+FORMS = {"many": (SAME(200, 77), 4, 2, 64), "few": ([(1, 300), (2, 290)], 4, 2, 128), "split": ([(1, 4096), (1, 3000)], 2, 1, 64)}
+
+
+def form(name, causal=True, seed=1):
+    lens, heads, kv, dim = FORMS[name]
+    t = Case(lens, heads, kv, dim, causal, seed=seed)
+    assert (t.workspace(False)[1] > 0) == (name == "split")
+    return t
+
+
+def put(t, **tensors):
+    for n, v in tensors.items():
+        t.v[n] = rounded(v, "bf16")
+        t.d[n].copy_(torch.from_numpy(t.v[n]))
+
+
+def scored(t, scores):
+    """Queries and keys whose score is `scores[j]` for each key j of a sequence, or that in bf16."""
+    q, k = np.zeros_like(t.v["q"]), np.zeros_like(t.v["k"])
+    q[:, :, 0] = 1.0 / t.scale if t.dim == 64 else 8.0
+    for c, d in zip(t.koff, t.koff[1:]):
+        k[c:d, :, 0] = scores[:d - c, None] * (1.0 if t.dim == 64 else 1.0 / (8.0 * t.scale))
+    put(t, q=q, k=k)
+
+
+def against_oracle(t):
+    """o and lse, where the oracle has NaNs too."""
+    o, lse, eo, el = S.attention(t.v["q"], t.v["k"], t.v["v"], t.qoff, t.koff, t.causal, t.scale)
+    for got, want, err in ((t.whole(t.d["o"]), o, eo), (host(t.lse), lse, el)):
+        ok = ~np.isnan(want)
+        assert np.array_equal(np.isnan(got), ~ok) and (np.abs(got - want)[ok] <= err[ok] + 1e-30).all()
+    return np.isnan(o)
+
+
+# ------------------------------------------------------- special values --
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("at,score", [(at, s) for s in (0.0, 400.0) for at in (0, 1010, 2000, 4095)])
+def test_a_special_value_in_one_split_reaches_the_row(bad, at, score):
+    """Whatever another split's score: its probability may be so small that 32 bits hold it as zero,
+    times which an infinity is a NaN."""
+    t = Case([(1, 4096)], 2, 1, 64, seed=5)
+    assert t.workspace(False)[1] > 0
+    scores = np.zeros(4096)
+    scores[1000] = score
+    scored(t, scores)
+    t.v["v"][at, 0, 3] = bad
+    t.d["v"].copy_(torch.from_numpy(t.v["v"]))
+    t.forward()
+    o = t.whole(t.d["o"])
+    assert not np.isfinite(o[:, :, 3]).any()
+    if score == 0.0:
+        assert np.array_equal(o[:, :, 3], np.full((1, 2), bad), equal_nan=True)
+    assert np.isfinite(np.delete(o, 3, 2)).all() and bool(t.lse.isfinite().all())
+
+
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("what", ["k", "v"])
+def test_special_values_against_the_oracle(name, what):
+    t = form(name, seed=7)
+    rng = np.random.default_rng(8)
+    for at in rng.integers(t.tk // 2, t.tk, 3):
+        t.v[what][at, 0, 5] = np.nan
+    t.d[what].copy_(torch.from_numpy(t.v[what]))
+    t.forward()
+    assert against_oracle(t).any()
