@@ -916,8 +916,9 @@ int op_attn_workspace_bytes(const ckpt_attn_desc *desc, int32_t backward, uint64
  * (f32 [heads, tq]), the logarithm of each row's sum of exponentials.  What a
  * query does not see has no part in its row, whatever values it holds.  The
  * exponentials are rounded to bf16 for their product with v and o divided by the
- * sum of the rounded ones (a row that sees one key gets its value, bit for bit).  A
- * re-run gives the same bits. */
+ * sum of the rounded ones (a row that sees one key gets its value, bit for bit).
+ * That product is summed in fp32: o is finite if the sum over the row's keys of
+ * exp(score - the row's largest) |v| is below 2^127.  A re-run gives the same bits. */
 int op_attn_forward(const ckpt_attn_desc *desc, const void *q, const void *k, const void *v,
                     const int32_t *qoff, const int32_t *koff, void *o, float *lse, void *workspace,
                     uint64_t workspace_bytes, void *stream);

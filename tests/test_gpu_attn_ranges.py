@@ -1,5 +1,5 @@
 """Attention over packed sequences (op_attn_*) where values go to their limits: special values, in split
-keys too.  Against the float64 oracle (oracle.seq)."""
+keys too, and values near the largest.  Against the float64 oracle (oracle.seq)."""
 import numpy as np
 import pytest
 
@@ -76,3 +76,22 @@ def test_special_values_against_the_oracle(name, what):
     t.d[what].copy_(torch.from_numpy(t.v[what]))
     t.forward()
     assert against_oracle(t).any()
+
+
+# --------------------------------------------------------- large values --
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("score", [0.0, 2.0, 5.1875, 40.0])
+def test_values_near_the_largest(name, score):
+    """One key's value near the largest of the type, its score above those that come by before it: o is
+    a weighted mean, so it is finite, as it is with exponentials of at most 1."""
+    t = form(name)
+    scores = np.zeros(4096)
+    scores[70] = score  # not in its wavefront's first turn
+    scored(t, scores)
+    v = t.v["v"] * 1e30
+    for c, d in zip(t.koff, t.koff[1:]):
+        v[c + 70] = 3.3e38 * np.sign(v[c + 70])
+    put(t, v=v)
+    t.forward()
+    t.check_forward()
+    assert np.abs(t.whole(t.d["o"])).max() > 1e34
