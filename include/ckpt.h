@@ -892,7 +892,8 @@ int op_embed_backward(const ckpt_embed_desc *desc, const void *ids, const void *
  * each; dim values a head (a multiple of 8, at most 128).  causal = 1: query i of
  * lq sees keys j <= i + lk - lq of lk (the queries are the last of the keys'
  * positions), else all.  A query that sees no key gets o = 0 and lse = -inf, and
- * adds to no gradient.
+ * adds to no gradient; one that sees keys, all with a score of -inf, gets NaNs (0 / 0),
+ * as do the gradients that it has a part in.
  * scale multiplies the scores (0: 1 / sqrt(dim)).  Elements from row to row ld?
  * (0: heads or kv_heads times dim) and from head to head hs? (0: dim) of q, k, v
  * and o; multiples of 8, addresses of 16 bytes.  g has o's strides; dq, dk and dv

@@ -28,8 +28,17 @@ using namespace at;
 // the average, and by 0.5e-7 with 0; of rows with hundreds by 3.7e-7 and 3.4e-7, the scores' own rounding.
 constexpr float ROOM = 8.f;
 
-// lse of a row with sum l, not 0
-__device__ __forceinline__ float lse_of(float base, float l) { return fmaf(base, LN2, logf(l * 0x1p8f)); }
+// The base of a row that sees keys is never below this, that of one that sees none is -infinity: both have l = 0 if
+// all scores are -infinity, but the first is no zero, it is 0 / 0.
+constexpr float LEAST = -3.402823466e38f;
+
+// lse of a row, and what its o is to be multiplied by, if times f / l otherwise
+__device__ __forceinline__ float lse_of(float base, float l) {
+  return l != 0.f ? fmaf(base, LN2, logf(l * 0x1p8f)) : base == -INFINITY ? -INFINITY : NAN;
+}
+__device__ __forceinline__ float over(float f, float base, float l) {
+  return l != 0.f ? f / l : base == -INFINITY ? 0.f : NAN;
+}
 
 struct Sums {
   float sc;  // of scores to exponents
@@ -60,8 +69,10 @@ struct Sums {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) lr = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[e], p[e + 1]}, ones, lr, false);
   }
-  // after the last key: l of the whole row, and the factor of o that goes with it
-  __device__ __forceinline__ float end() {
+  // after the last key: l of the whole row, and the factor of o that goes with it.  sees: the row sees a key (of a
+  // row's parts, one says so)
+  __device__ __forceinline__ float end(bool sees) {
+    if (sees) base = fmaxf(base, LEAST);
     l = halves_add(l);
     lr = halves_add(lr);
     return l == 0.f ? 0.f : l / lr;
@@ -127,8 +138,8 @@ __device__ __forceinline__ void finish(const AttnArgs &A, int split, int head, i
     part(A.po + p * A.dim, factor);
     return;
   }
-  if (sums) A.lse[at_row] = l == 0.f ? -INFINITY : lse_of(base, l);
-  part(A.o + token * A.ldo + head * A.hso, l == 0.f ? 0.f : factor / l);
+  if (sums) A.lse[at_row] = lse_of(base, l);
+  part(A.o + token * A.ldo + head * A.hso, over(factor, base, l));
 }
 
 // A wavefront's 32 rows as 32 keys after the other go by; of o it forms 32 N columns.
@@ -239,7 +250,7 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
                 });
   if (begin < end && special)
     add_special(r.o, vp, A.ldv, A.dim, scrubbed * BN, min(end * BN, lk), false, [&](int j) { return j < y.lim; });
-  const float factor = r.z.end();
+  const float factor = r.z.end(b.split == 0 && y.lim > 0);
   if (y.valid)
     finish(A, b.split, y.head, y.sq.q0 + y.token, r.z.base, r.z.l, factor, true,
            [&](auto *row, float scale) { store_row(row, r.o, scale, A.dim); });
@@ -288,7 +299,7 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       *place(part, columns + t, c) = make_float4(r.o[t][4 * c], r.o[t][4 * c + 1], r.o[t][4 * c + 2], r.o[t][4 * c + 3]);
-  const float factor = r.z.end();
+  const float factor = r.z.end(b.split == 0 && part == 0 && y.lim > 0);
   if (columns == 0 && lane < 32) {
     bases[part][lane] = r.z.base;
     ls[part][lane] = r.z.l;
@@ -339,8 +350,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   float top = base;
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (top == -INFINITY) top = 0.f;
-  const float f = exp2_fast(base - top);  // 0 for a split without keys, which left zeros
+  const float f = exp2_fast(base - (top == -INFINITY ? 0.f : top));  // 0 for a split without keys, which left zeros
   l *= f;                                 // a NaN of a split stays one
 #pragma unroll
   for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
@@ -357,9 +367,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) s[k] = xor_add<32>(xor_add<16>(s[k]));
-  if (lane == 0) A.lse[at] = l == 0.f ? -INFINITY : lse_of(top, l);
+  if (lane == 0) A.lse[at] = lse_of(top, l);
   if (ok && quarter == 0) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = over(1.f, top, l);
     bf16x8 r;
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k] = (__bf16)(s[k] * inv);

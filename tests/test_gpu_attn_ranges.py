@@ -1,5 +1,5 @@
 """Attention over packed sequences (op_attn_*) where values go to their limits: special values, in split
-keys too, and values near the largest.  Against the float64 oracle (oracle.seq)."""
+keys too, values near the largest, and scores of -inf.  Against the float64 oracle (oracle.seq)."""
 import numpy as np
 import pytest
 
@@ -95,3 +95,70 @@ def test_values_near_the_largest(name, score):
     t.forward()
     t.check_forward()
     assert np.abs(t.whole(t.d["o"])).max() > 1e34
+
+
+# ------------------------------------------------------ scores of -inf --
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_whose_scores_are_all_minus_infinity(name, causal):
+    """exp(-inf) over a sum of such: NaN, and so are the gradients of what such a row sees; what sees no
+    such score is as without them."""
+    t = form(name, causal)
+    k, q = t.v["k"].copy(), t.v["q"].copy()
+    k[:, :, 0] = 1.0
+    rows = [int(b) - 1 for b in t.qoff[1:2]]  # the first sequence's last query
+    for i in rows:
+        q[i] = 0.0
+        q[i, :, 0] = -np.inf
+    t.v["k"], t.v["q"] = k, q
+    for n in "qk":
+        t.d[n].copy_(torch.from_numpy(t.v[n]))
+    t.forward()
+    assert against_oracle(t)[rows].all()
+    t.backward()
+    dq, dk, dv = (t.whole(x) for x in t.grads)
+    n = t.koff[1]
+    assert np.isnan(dq[rows]).all() and np.isnan(dv[:n]).all() and np.isnan(dk[:n]).all()
+    assert np.isfinite(np.delete(dq, rows, 0)).all() and np.isfinite(dv[n:]).all() and np.isfinite(dk[n:]).all()
+
+
+@pytest.mark.parametrize("name", FORMS)
+def test_some_scores_of_minus_infinity(name):
+    """They have no part, however many tiles or splits hold nothing else; rows that see nothing else are NaN."""
+    t = form(name)
+    first = {"many": 130, "few": 65, "split": 1100}[name]
+    q, k = np.abs(t.v["q"]) + 0.25, t.v["k"].copy()
+    t.v["q"] = rounded(q, "bf16")
+    for c, d in zip(t.koff, t.koff[1:]):
+        k[c:min(d, c + first), :, 0] = -np.inf
+    t.v["k"] = k
+    for n in "qk":
+        t.d[n].copy_(torch.from_numpy(t.v[n]))
+    t.forward()
+    o, lse = t.whole(t.d["o"]), host(t.lse)
+    i = 0
+    for a, b, c, d in zip(t.qoff, t.qoff[1:], t.koff, t.koff[1:]):
+        for r in range(a, b):
+            lim = r - a + (d - c) - (b - a) + 1
+            if lim <= first:
+                assert np.isnan(o[r]).all() and np.isnan(lse[:, r]).all()
+                continue
+            for h in range(t.heads):
+                kh = h // (t.heads // t.kv)
+                keys, v, query = t.v["k"][c + first:c + lim, kh], t.v["v"][c + first:c + lim, kh], t.v["q"][r, h]
+                e = keys @ query * t.scale
+                p = np.exp(e - e.max())
+                # a score is a sum of dim products; weights and the output are rounded to bf16
+                rel = (t.dim + 16) * S.U24 * 2 * ((np.abs(keys) @ query).max() * t.scale + abs(e.max())) + (lim + 64) * S.U24
+                want, mag = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+                assert (np.abs(o[r, h] - want) <= (S.U16 + 2 * rel) * mag + 2 * S.U16 * np.abs(want)).all()
+                log = e.max() + np.log(p.sum())
+                assert abs(lse[h, r] - log) <= rel + 4 * S.U24 * abs(log)
+            i += 1
+    assert i > 0
+
+
+def test_rows_that_see_no_key_are_zeros_beside_them():
+    t = Case([(9, 4), (1, 0), (1, 5)], 2, 1, 64)
+    t.check()
+    assert not t.whole(t.d["o"])[[0, 1, 2, 3, 4, 9]].any() and bool(t.lse[:, [0, 1, 2, 3, 4, 9]].isneginf().all())
