@@ -919,7 +919,8 @@ int op_attn_workspace_bytes(const ckpt_attn_desc *desc, int32_t backward, uint64
  * exponentials are rounded to bf16 for their product with v and o divided by the
  * sum of the rounded ones (a row that sees one key gets its value, bit for bit).
  * That product is summed in fp32: o is finite if the sum over the row's keys of
- * exp(score - the row's largest) |v| is below 2^127.  A re-run gives the same bits. */
+ * exp(score - the row's largest) |v| is below 2^127.  Scores are fp32 and may be
+ * as large as 2^126.  A re-run gives the same bits. */
 int op_attn_forward(const ckpt_attn_desc *desc, const void *q, const void *k, const void *v,
                     const int32_t *qoff, const int32_t *koff, void *o, float *lse, void *workspace,
                     uint64_t workspace_bytes, void *stream);
@@ -927,7 +928,9 @@ int op_attn_forward(const ckpt_attn_desc *desc, const void *q, const void *k, co
 /* op_attn_backward -- from o and lse that op_attn_forward left: with p = exp(scale
  * q k^T - lse) and ds = p (g v^T - sum(g o)) (both rounded to bf16 for the
  * products), dq = scale ds k, dk = scale ds^T q and dv = p^T g, the last two added
- * up over the query heads that share a key head. */
+ * up over the query heads that share a key head.  lse is fp32, so p is off by up to
+ * |lse| 2^-22 of itself: less than its rounding to bf16 up to |lse| = 2^13, and all of
+ * it from 2^22 on, where gradients are not to be used. */
 int op_attn_backward(const ckpt_attn_desc *desc, const void *g, const void *q, const void *k,
                      const void *v, const void *o, const float *lse, const int32_t *qoff,
                      const int32_t *koff, void *dq, void *dk, void *dv, void *workspace,

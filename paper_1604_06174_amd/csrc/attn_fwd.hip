@@ -40,9 +40,16 @@ __device__ __forceinline__ float over(float f, float base, float l) {
   return l != 0.f ? f / l : base == -INFINITY ? 0.f : NAN;
 }
 
+//
+// An exponent is score sc + add, in one operation.  Where the base is large that will not do: the product
+// score sc, which the base comes from, and the one inside the fused operation differ by half a step of fp32 (1/4 at
+// 2^22, 128 at 2^31), so an exponential may overflow or all of a row's be zeros.  If it is so for a row of the
+// wavefront, exponents are formed apart (a test of a scalar for others).
 struct Sums {
   float sc;  // of scores to exponents
   float base = -INFINITY, l = 0.f, lr = 0.f, top = 0.f;
+  float add = 0.f;
+  bool large = false;
 
   __device__ __forceinline__ explicit Sums(float scale) : sc(scale) {}
   // does a row of the wavefront have to move its base for scores up to `score`?
@@ -57,11 +64,17 @@ struct Sums {
     base = to;
     l *= f;
     lr *= f;
+    const float from = base == -INFINITY ? 0.f : base;
+    large = __any(fabsf(from) >= 0x1p22f);
+    add = large ? 0.f : -ROOM - from;
     return f;
   }
-  __device__ __forceinline__ float exponential(float score) const {
-    return exp2_fast(fmaf(score, sc, base == -INFINITY ? 0.f : -ROOM - base));
+  __device__ __forceinline__ float apart(float score) const {
+#pragma clang fp contract(off)
+    const float e = score * sc;
+    return e - (base == -INFINITY ? 0.f : base) - ROOM;
   }
+  __device__ __forceinline__ float exponential(float score) const { return exp2_fast(fmaf(score, large ? 1.f : sc, add)); }
   // to lr: eight rounded exponentials
   __device__ __forceinline__ void add_rounded(bf16x8 p) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -177,6 +190,10 @@ struct Rows {
       for (int t = 0; t < N; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= f;
+    }
+    if (z.large) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = z.apart(s[0][i]);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {

@@ -1,5 +1,5 @@
 """Attention over packed sequences (op_attn_*) where values go to their limits: special values, in split
-keys too, values near the largest, and scores of -inf.  Against the float64 oracle (oracle.seq)."""
+keys too, values near the largest, scores of -inf and huge ones.  Against the float64 oracle (oracle.seq)."""
 import numpy as np
 import pytest
 
@@ -162,3 +162,62 @@ def test_rows_that_see_no_key_are_zeros_beside_them():
     t = Case([(9, 4), (1, 0), (1, 5)], 2, 1, 64)
     t.check()
     assert not t.whole(t.d["o"])[[0, 1, 2, 3, 4, 9]].any() and bool(t.lse[:, [0, 1, 2, 3, 4, 9]].isneginf().all())
+
+
+# --------------------------------------------------------- huge scores --
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("size", [300.0, 3000.0, 20000.0, 30000.0, 1e8, 1e15])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_huge_scores(name, size, sign):
+    """Scores that 32 bits hold to many whole numbers only, up to 1e31: equal ones have equal
+    weights, those far below have none, and nothing overflows."""
+    t = form(name)
+    q, k = np.full_like(t.v["q"], size), np.full_like(t.v["k"], sign * size)
+    rng = np.random.default_rng(3)
+    low = rng.random(t.tk) < 0.5
+    low[t.koff[:-1]] = False  # a key that every query sees
+    k[low] *= -sign if sign > 0 else 4.0  # all below the others
+    put(t, q=q, k=k)
+    t.forward()
+    o, lse = t.whole(t.d["o"]), host(t.lse)
+    top = t.dim * t.v["q"][0, 0, 0] * t.v["k"][t.koff[0], 0, 0] * t.scale
+    for a, b, c, d in zip(t.qoff, t.qoff[1:], t.koff, t.koff[1:]):
+        for r in range(a, b):
+            lim = r - a + (d - c) - (b - a) + 1
+            v = np.repeat(t.v["v"][c:c + lim][~low[c:c + lim]], t.heads // t.kv, 1)
+            # weights and the output rounded to bf16, fp32 sums of at most 4096 values
+            want, mag = v.mean(0), np.abs(v).mean(0)
+            assert (np.abs(o[r] - want) <= S.U16 * (mag + 2 * np.abs(want)) + (lim + 64) * S.U24 * mag).all()
+            # a score is a sum of dim products, scaled and taken to base 2 and back
+            assert (np.abs(lse[:, r] - (top + np.log(len(v)))) <= (t.dim + 8) * S.U24 * abs(top) + 1e-4).all()
+
+
+@pytest.mark.parametrize("size", [1.0, 30000.0, 1e8])
+def test_huge_scores_beside_rows_that_see_nothing(size):
+    """In one wavefront: rows without keys, rows of small scores, and rows of huge ones."""
+    t = Case([(100, 61), (70, 70)], 2, 2, 64)
+    q = t.v["q"].copy()
+    q[::3] *= size
+    put(t, q=q)
+    t.forward()
+    o, lse = t.whole(t.d["o"]), host(t.lse)
+    assert not o[:39].any() and np.isneginf(lse[:, :39]).all()
+    assert np.isfinite(o).all() and np.isfinite(lse[:, 39:]).all()
+    want, wl, eo, el = S.attention(t.v["q"], t.v["k"], t.v["v"], t.qoff, t.koff, True, t.scale)
+    small = np.arange(170) % 3 != 0
+    assert (np.abs(o - want)[small] <= eo[small] + 1e-30).all()
+    some = np.flatnonzero(small)[np.flatnonzero(small) >= 39]
+    assert (np.abs(lse[:, some] - wl[:, some]) <= el[:, some]).all()
+
+
+@pytest.mark.parametrize("size", [3.0, 30.0, 100.0, 300.0])
+def test_gradients_of_large_scores(size):
+    """Of a row that sees one key p is 1, off by the roundings of its lse: half a step of fp32 each where it is
+    stored and taken to base 2 and back, and of the score, below 4 of them.  dv = p g."""
+    t = Case(SAME(*[1] * 40), 2, 2, 64)
+    put(t, q=np.full_like(t.v["q"], size), k=np.full_like(t.v["k"], size))
+    t.forward()
+    t.backward()
+    g, lse = t.v["g"], host(t.lse).T[:, :, None]
+    # p and dv are rounded to bf16
+    assert (np.abs(t.whole(t.grads[2]) - g) <= (lse * 4 * S.U24 + 2.1 * S.U16) * np.abs(g)).all()
