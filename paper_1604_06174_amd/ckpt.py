@@ -848,21 +848,26 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
 # given as plain bytes
 _SEQ_TYPES = {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16, TYPE_E4M3: torch.float8_e4m3fn}
 _IDS = torch.int32, torch.int64
+_VECTOR = object()  # fp32 values side by side
 
 
 def _places(name, *args):
-    """The addresses of (x, arg, type)s.  Tensors have to be on the current device and of their type
-    if they are floating-point, integers of theirs side by side if that is an integer one; addresses
-    and other memory are taken as they are."""
+    """The addresses of (x, arg, type)s.  Tensors have to be on the current device and of their type;
+    ids and offsets, vectors and workspaces (None) side by side.  Floating-point ones may also be given as
+    memory: bytes, or integers of their size.  Addresses are taken as they are."""
     out, here = [], None
     for x, arg, want in args:
         if not isinstance(x, torch.Tensor):
             out.append(_addr(x))
             continue
         t = x.dtype
-        if want in _IDS and not (t is want and x.is_contiguous()):
+        if want is _VECTOR or want is None:
+            if not x.is_contiguous():
+                raise CkptError(E_INVALID, f"{name}({arg}): a tensor of strides {x.stride()}, not contiguous")
+            want = _F32 if want is _VECTOR else t
+        elif want in _IDS and not (t is want and x.is_contiguous()):
             raise CkptError(E_INVALID, f"{name}({arg}): {t} of strides {x.stride()}, not contiguous {want}")
-        if t is not want and t.is_floating_point and want is not None:
+        if t is not want and (t.is_floating_point or t.itemsize not in (1, want.itemsize)):
             raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {t}, described as {want}")
         if x.get_device() != here:
             here = torch.cuda.current_device() if x.is_cuda else None
@@ -887,15 +892,15 @@ def rms_desc(rows, c, xtype=TYPE_BF16, htype=None, ytype=None, gtype=None, dtype
 def op_rms_forward(desc: RmsDesc, x, w, y, st, res=None, h=None, ys=None, stream=None):
     ht = _SEQ_TYPES.get(desc.htype)
     px, pr, pw, ph, py, pq, ps = _places(
-        "op_rms_forward", (x, "x", _SEQ_TYPES.get(desc.xtype)), (res, "res", ht), (w, "w", _F32), (h, "h", ht),
-        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _F32), (st, "st", _F32))
+        "op_rms_forward", (x, "x", _SEQ_TYPES.get(desc.xtype)), (res, "res", ht), (w, "w", _VECTOR), (h, "h", ht),
+        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _VECTOR), (st, "st", _VECTOR))
     _check(_lib.op_rms_forward(desc, px, pr, pw, ph, py, pq, ps, _s(stream)))
 
 
 def op_rms_apply(desc: RmsDesc, h, st, w, y, ys=None, stream=None):
     ph, ps, pw, py, pq = _places(
-        "op_rms_apply", (h, "h", _SEQ_TYPES.get(desc.htype)), (st, "st", _F32), (w, "w", _F32),
-        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _F32))
+        "op_rms_apply", (h, "h", _SEQ_TYPES.get(desc.htype)), (st, "st", _VECTOR), (w, "w", _VECTOR),
+        (y, "y", _SEQ_TYPES.get(desc.ytype)), (ys, "ys", _VECTOR))
     _check(_lib.op_rms_apply(desc, ph, ps, pw, py, pq, _s(stream)))
 
 
@@ -909,7 +914,7 @@ def op_rms_backward(desc: RmsDesc, g, h, st, w, d, dw, workspace, workspace_byte
     dt = _SEQ_TYPES.get(desc.dtype)
     pg, pe, ph, ps, pw, pd, pdw, ws = _places(
         "op_rms_backward", (g, "g", _SEQ_TYPES.get(desc.gtype)), (gh, "gh", dt), (h, "h", _SEQ_TYPES.get(desc.htype)),
-        (st, "st", _F32), (w, "w", _F32), (d, "d", dt), (dw, "dw", _F32), (workspace, "workspace", None))
+        (st, "st", _VECTOR), (w, "w", _VECTOR), (d, "d", dt), (dw, "dw", _VECTOR), (workspace, "workspace", None))
     _check(_lib.op_rms_backward(desc, pg, pe, ph, ps, pw, pd, pdw, ws, _nbytes(workspace_bytes), _s(stream)))
 
 
@@ -962,7 +967,7 @@ def op_attn_forward(desc: AttnDesc, q, k, v, qoff, koff, o, lse, workspace=None,
     bf, i32 = torch.bfloat16, torch.int32
     pq, pk, pv, pa, pb, po, pl, ws = _places(
         "op_attn_forward", (q, "q", bf), (k, "k", bf), (v, "v", bf), (qoff, "qoff", i32), (koff, "koff", i32), (o, "o", bf),
-        (lse, "lse", _F32), (workspace, "workspace", None))
+        (lse, "lse", _VECTOR), (workspace, "workspace", None))
     _check(_lib.op_attn_forward(desc, pq, pk, pv, pa, pb, po, pl, ws, _nbytes(workspace_bytes), _s(stream)))
 
 
@@ -970,7 +975,7 @@ def op_attn_backward(desc: AttnDesc, g, q, k, v, o, lse, qoff, koff, dq, dk, dv,
                      stream=None):
     bf, i32 = torch.bfloat16, torch.int32
     pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, ws = _places(
-        "op_attn_backward", (g, "g", bf), (q, "q", bf), (k, "k", bf), (v, "v", bf), (o, "o", bf), (lse, "lse", _F32),
+        "op_attn_backward", (g, "g", bf), (q, "q", bf), (k, "k", bf), (v, "v", bf), (o, "o", bf), (lse, "lse", _VECTOR),
         (qoff, "qoff", i32), (koff, "koff", i32), (dq, "dq", bf), (dk, "dk", bf), (dv, "dv", bf),
         (workspace, "workspace", None))
     _check(_lib.op_attn_backward(desc, pg, pq, pk, pv, po, pl, pa, pb, pdq, pdk, pdv, ws, _nbytes(workspace_bytes),
