@@ -847,7 +847,7 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
 # tensors by type code (an unknown one is the library's to refuse); an 8-bit output may also be
 # given as plain bytes
 _SEQ_TYPES = {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16, TYPE_E4M3: torch.float8_e4m3fn}
-_IDS = torch.int32, torch.int64
+_IDS = _I32, _I64 = torch.int32, torch.int64
 _VECTOR = object()  # fp32 values side by side
 
 
@@ -861,20 +861,27 @@ def _places(name, *args):
             out.append(_addr(x))
             continue
         t = x.dtype
-        if want is _VECTOR or want is None:
-            if not x.is_contiguous():
-                raise CkptError(E_INVALID, f"{name}({arg}): a tensor of strides {x.stride()}, not contiguous")
-            want = _F32 if want is _VECTOR else t
-        elif want in _IDS and not (t is want and x.is_contiguous()):
-            raise CkptError(E_INVALID, f"{name}({arg}): {t} of strides {x.stride()}, not contiguous {want}")
-        if t is not want and (t.is_floating_point or t.itemsize not in (1, want.itemsize)):
-            raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {t}, described as {want}")
-        if x.get_device() != here:
+        if want is _VECTOR:
+            if t is not _F32 or not x.is_contiguous():
+                _as_memory(name, arg, x, _F32, True)
+        elif t is not want or want is _I32 or want is _I64:
+            _as_memory(name, arg, x, want, want is None or want in _IDS)
+        device = x.get_device()
+        if device != here:
             here = torch.cuda.current_device() if x.is_cuda else None
-            if x.get_device() != here:
+            if device != here:
                 raise CkptError(E_INVALID, f"{name}({arg}): a tensor on {x.device}, not on the current device")
         out.append(x.data_ptr())
     return out
+
+
+def _as_memory(name, arg, x, want, dense):
+    """The checks of _places that a tensor of its type without strides need not pass."""
+    t = x.dtype
+    if dense and not x.is_contiguous():
+        raise CkptError(E_INVALID, f"{name}({arg}): a tensor of strides {x.stride()}, not contiguous")
+    if want is not None and t is not want and (want in _IDS or t.is_floating_point or t.itemsize not in (1, want.itemsize)):
+        raise CkptError(E_INVALID, f"{name}({arg}): a tensor of {t}, described as {want}")
 
 
 def rms_desc(rows, c, xtype=TYPE_BF16, htype=None, ytype=None, gtype=None, dtype=None, qgroup=0, ldx=0, ldh=0, ldy=0,
