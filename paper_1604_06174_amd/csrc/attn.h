@@ -86,10 +86,11 @@ __device__ __forceinline__ int wave_add(int v) {
 // Up to 64 sequences, a lane each, are ordered by their tiles' work, longest first: a causal tile's
 // is its place in its sequence (of queries with the keys before them, of keys with the queries
 // behind them), so the tiles of a level w or above are counted, sum over the sequences of how far they
-// reach past w, and the level is searched for.  Then no long tile is left to the end, and no
-// workgroup is without one.
+// reach past w, and the level is searched for.  Then no long tile is left to the end.  A launch has
+// workgroups for one more tile a sequence than its rows may fill; those without a tile come last.
 // More sequences take the tiles from off[s] per / size + s on each: as many as its rows can take
-// whatever their number, so a tile's sequence is found without adding lengths up.
+// whatever their number, so a tile's sequence is found without adding lengths up.  Tiles then come in
+// their sequences' order, those that rows do not fill among them.
 template <bool QUERIES>
 __device__ __forceinline__ bool find_tile(const AttnArgs &A, int per, int size, int tiles, int index, Sequence &q) {
   const int lane = threadIdx.x & 63;
