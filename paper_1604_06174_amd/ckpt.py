@@ -848,6 +848,7 @@ def op_dropout(rows, cols, x, y, drop, res=None, xtype=None, ytype=None, ldx=0, 
 # given as plain bytes
 _SEQ_TYPES = {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16, TYPE_E4M3: torch.float8_e4m3fn}
 _IDS = _I32, _I64 = torch.int32, torch.int64
+_Tensor = torch.Tensor
 _VECTOR = object()  # fp32 values side by side
 
 
@@ -857,7 +858,7 @@ def _places(name, *args):
     memory: bytes, or integers of their size.  Addresses are taken as they are."""
     out, here = [], None
     for x, arg, want in args:
-        if not isinstance(x, torch.Tensor):
+        if not isinstance(x, _Tensor):
             out.append(_addr(x))
             continue
         t = x.dtype
