@@ -5,10 +5,12 @@
 // the keys come by, k_attn_dkv keeps 32 keys and lets the queries come by (p and ds are formed in
 // both: seven products instead of five).
 //
-// Both are bound by the vector and matrix units together, as the forward is: 8192 causal tokens, 16/4
-// heads of 128: dq 420 us, dk and dv 610 and 23 for the query heads' parts, 675 TFLOP/s of the
-// five products or 945 of the seven that run (the library's largest bf16 products reach 1300); 8192
-// tokens in 19 sequences, 16 heads of 64: 41 and 51 us.
+// Both are bound as the forward is, by the order within a wavefront, with two of them on a SIMD (wide heads): of
+// the cycles that a compute unit is busy, matrix instructions take 56% in dq and 48% in dk and dv, vector ones 30% and
+// more (exponentials), LDS reads 28% and 36%.  8192 causal tokens, 16/4 heads of 128: dq 409 us, dk and dv 613 and 23
+// for the query heads' parts, 1018 in a stream of calls, 675 TFLOP/s of the five products or 945 of the seven that
+// run (the library's largest bf16 products reach 1300); 8201 tokens in 19 sequences, 16 heads of 64: 51 and 51, 95
+// in a stream of calls.
 #include "attn.h"
 #include "common.h"
 
@@ -130,7 +132,8 @@ static __device__ __align__(16) const float g_infinity[64] = {
     CKPT_INF16, CKPT_INF16, CKPT_INF16, CKPT_INF16};
 
 // dk and dv: the wavefront's keys stay in registers and the workgroup's values in LDS, read as they are
-// needed, for dk, dv, p and ds fill the registers; queries, g, lse and delta come by in tiles of 32.
+// needed, for dk, dv, p and ds fill the registers (of wide heads five go to memory, none of them in the loop
+// over whole tiles); queries, g, lse and delta come by in tiles of 32.
 // A key head's query heads are taken one after the other, or dealt to `parts` workgroups.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_dkv(AttnArgs A) {

@@ -236,9 +236,10 @@ __device__ __forceinline__ int each_tile(const Loader<D, BN, 256> &kload, const 
 }
 
 // Four wavefronts of 32 rows share tiles of 32 keys, which leaves room for three of them on each SIMD.
-// Bound by the vector and matrix units together, and by power (16384 tokens, 16/4 heads of 128 in seven
-// sequences: 230 us, 880 TFLOP/s of the visible products, at 2.0 GHz; the library's largest bf16 products
-// reach 1300).  Tiles of 64 keys with two wavefronts took 4% longer, and so did the scores, exponentials
+// 16384 tokens, 16/4 heads of 128 in seven sequences: 235 us, 860 TFLOP/s of the visible products (the library's
+// largest bf16 products reach 1300).  Bound by a wavefront's own order, scores, exponentials, values, which three on
+// a SIMD cover in part: of the cycles that a compute unit is busy, vector instructions take 64%, matrix ones 45%,
+// LDS reads 23%, without a conflict.  Tiles of 64 keys with two wavefronts took 4% longer, and so did the scores, exponentials
 // and values of three turns side by side; 64 rows a wavefront, one a SIMD, 25%.
 template <int D>
 __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
@@ -275,8 +276,8 @@ __global__ __launch_bounds__(256, 3) void k_attn_many(AttnArgs A, int tiles) {
 
 // Four wavefronts with the same 32 rows and tiles of 64 keys: two take 32 of the keys each, and half of o's
 // columns (forming the same scores twice, which costs a call that HBM bounds nothing), and the sums over the keys
-// are joined at the end.  Bound by HBM: 16 single tokens, 32/8 heads of 128, up to 8192 keys, 66 us in
-// all, 4.6 TB/s.  With tiles of 128 keys, a quarter of them a wavefront's, one workgroup fits a compute unit,
+// are joined at the end.  Bound by HBM: 16 single tokens, 32/8 heads of 128, up to 8192 keys, 64 us in
+// all, 4.7 TB/s.  With tiles of 128 keys, a quarter of them a wavefront's, one workgroup fits a compute unit,
 // and its start and end (7 us) are not covered: 3 us more.
 template <int D>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs A, int tiles) {
@@ -394,9 +395,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs A) {
   }
 }
 
-// Up to 32 rows a sequence on the average go to k_attn_few.  64 sequences of 1024 keys, 16 heads of 64: 32
-// rows each 60 us (by k_attn_many 58), 64 each 103 (62); one token, 8 heads of 128 against 2048 keys 13 (16),
-// 16 tokens of 32/8 heads against up to 8192 73 (75 to 81).
+// Up to 32 rows a sequence on the average go to k_attn_few.  64 sequences of 1024 keys, 16 heads of 64: 8 or 32
+// rows each 61 us (by k_attn_many 57), 64 each 103 (61); one token, 8 heads of 128 against 2048 keys 13 (16),
+// 16 tokens of 32/8 heads against up to 8192 56 (62).
 bool few_rows(const AttnArgs &a) { return a.tq * a.rep <= int64_t(32) * a.seqs; }
 
 template <int D>
@@ -416,9 +417,9 @@ void forward(hipStream_t s, const AttnArgs &a) {
 
 // Workgroups for one another's keys where the rows alone make less than three for each compute
 // unit; a split is 256 keys at least of a sequence of the average length.  768: 16 single tokens,
-// 32/8 heads of 128, against up to 8192 keys 66 us, against 4096 each 64; 512: 73, for the longest sequences
-// end last, and 60; 1024: 72 and 60.  256 keys: one token of 8 heads against 2048 13 us, of 32/8 heads
-// against 16384 26; 512 keys: 17 and 23.
+// 32/8 heads of 128, against up to 8192 keys (three batches) 56, 56 and 58 us; 512: 68, 66 and 68, for the longest
+// sequences end last; 1024: 59, 59 and 61.  Against 4096 keys each it is 64, 60 and 62, but lengths are seldom
+// equal.  256 keys: one token of 8 heads against 2048 13 us, of 32/8 heads against 16384 26; 512 keys: 17 and 23.
 int attn_splits(const AttnArgs &a) {
   const int bm = few_rows(a) ? 32 : 128;
   const int64_t work = (a.tq * a.rep / bm > a.seqs ? a.tq * a.rep / bm : a.seqs) * a.kv_heads;

@@ -306,7 +306,8 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_rms_bwd(RmsBwdArgs A) {
 }
 
 // dw = the workgroups' records added up: 32 columns a workgroup, each of 32 half wavefronts every 32nd
-// record, sixteen in flight, then the 32 sums in order
+// record, sixteen in flight, then the 32 sums in order: a chain of at most rows / teams in a team, its workgroup's
+// four teams, 48 records and 32 sums
 __global__ __launch_bounds__(1024) void k_rms_dw(const float *part, int groups, int c, int cpad, float *dw) {
   constexpr int AHEAD = 16;
   __shared__ float red[32][32];
@@ -333,7 +334,9 @@ __global__ __launch_bounds__(1024) void k_rms_dw(const float *part, int groups, 
 
 // A row's team and vectors a thread.  At 134 MB a tensor of 16 bits: rows of 2048 by a wavefront with
 // four vectors a thread 55 us forward and 79 backward, by a workgroup with one 51 and 58; rows of
-// 8192 by 256 threads with four 54 and 84, by 1024 with one 49 and 61.
+// 8192 by 256 threads with four 54 and 84, by 1024 with one 49 and 61.  Rows above 8192 columns leave the backward
+// 128 registers a thread, and with mixed types 2 to 38 more go to memory: 2048 x 16384, g fp32, h and d bf16 82 us
+// (4.1 TB/s), g and h bf16, d fp32 94 (4.3); all of them bf16, with none, 58 (4.7).
 template <typename F>
 void with_team(int c, F &&f) {
   using std::integral_constant;
