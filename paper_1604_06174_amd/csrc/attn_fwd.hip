@@ -32,7 +32,8 @@ constexpr float ROOM = 8.f;
 // all scores are -infinity, but the first is no zero, it is 0 / 0.
 constexpr float LEAST = -3.402823466e38f;
 
-// lse of a row, and what its o is to be multiplied by, if times f / l otherwise
+// lse of a row, and what its o is to be multiplied by for the mean of the values, f / l as a rule
+static_assert(ROOM == 8.f, "l is 2^-8 times the sum relative to the base");
 __device__ __forceinline__ float lse_of(float base, float l) {
   return l != 0.f ? fmaf(base, LN2, logf(l * 0x1p8f)) : base == -INFINITY ? -INFINITY : NAN;
 }
@@ -40,7 +41,6 @@ __device__ __forceinline__ float over(float f, float base, float l) {
   return l != 0.f ? f / l : base == -INFINITY ? 0.f : NAN;
 }
 
-//
 // An exponent is score sc + add, in one operation.  Where the base is large that will not do: the product
 // score sc, which the base comes from, and the one inside the fused operation differ by half a step of fp32 (1/4 at
 // 2^22, 128 at 2^31), so an exponential may overflow or all of a row's be zeros.  If it is so for a row of the
